@@ -215,6 +215,85 @@ int pafu_chunk_attention_fp8(void* stream, const void* Q, int Lq, const void* Kc
                              int v_scale_log2, void* O, int out_dtype, void* workspace, size_t workspace_bytes);
 
 /* ------------------------------------------------------------------------------------------
+ * Paged K/V cache: one pool of pages shared by several requests (beyond the paper, whose cache belongs to one video).
+ *
+ * The pool is [n_pages, page_size, N_kv, D] for K and the same for V, page_size a power of two from 8 to 4096, D 64 or
+ * 128, stored as PAFU_BF16 or PAFU_FP8_E4M3 (one power-of-two scale per tensor, as above).  Strides ld_page, ld_token and
+ * ld_head are given in ELEMENTS and are shared by K and V; D elements are contiguous.  Heads may lie inside a token
+ * (ld_token >= N_kv * ld_head) or tokens inside a head (ld_head >= page_size * ld_token), and K and V pages may alternate
+ * in one slab; two elements of the pool never share a place (PAFU_ERR_SHAPE).  The stride of an axis of length one is
+ * not read.
+ * Request b's tokens lie in order on the pages block_table[b * ld_table + 0, 1, ...]; the slot of a token is
+ * page * page_size + its place on the page.  In a pool with heads inside tokens and no gaps slots are row numbers of the
+ * pool seen as [n_pages * page_size, N_kv, D]: pafu_chunk_attention_gather and pafu_compact_kv take them as ids.
+ * All lengths, tables and slots are int32 on the device and are read when the kernels run, so that a captured graph
+ * follows them; nothing in them can make a kernel leave its buffers (what is out of range takes no part, as said below).
+ * Shapes are what the launch is sized for: requests of a padded batch have length 0.  At most
+ * PAFU_PAGED_MAX_REQUESTS requests a call.  B == 0 is a no-op.
+ */
+#define PAFU_PAGED_MAX_REQUESTS 8192
+
+/* pafu_paged_tables - pages and slots for the tokens that each request is about to append.
+ *   have(b) = ceil(kv_len[b] / page_size), want(b) = ceil((kv_len[b] + new_len[b]) / page_size)
+ *   block_table[b, have(b) + i] = free_pages[at(b) + i]    0 <= i < want(b) - have(b)
+ *   at(b)        = *free_start + the pages that requests before b take (free_start NULL: 0)
+ *   *free_end    = *free_start + the pages that all requests take: the next call's free_start
+ *   row_start[b] = the new tokens of the requests before b (b = 0 .. B): the first row of request b
+ *   slots[row_start[b] + j] = slot of request b's token kv_len[b] + j, 0 <= j < new_len[b]
+ *   kv_len_out[b] = kv_len[b] + new_len[b]
+ *   kv_len, new_len : [B]   free_pages : [n_free]   block_table : [B, max_pages], in and out, other entries unchanged
+ *   slots : [max_slots]; rows behind the last one get -1, rows that do not fit are left out
+ *   row_start : [B + 1]   kv_len_out : [B]   free_start, free_end : one int32 each (4-byte aligned)
+ * A page that the list does not hold (*free_end > n_free says so) is entered as -1; one beyond max_pages is not entered
+ * but counted; slots of either are -1.  Negative lengths count as 0, sums saturate at 2^31 - 1.
+ * pafu_paged_slots - the same slots for tokens that have their pages: request b's tokens start[b] .. start[b] +
+ * count[b] - 1.  A token whose page is negative or beyond max_pages gets -1.
+ */
+int pafu_paged_tables(void* stream, const int* kv_len, const int* new_len, int B, const int* free_pages, int n_free,
+                      const int* free_start, int page_size, int* block_table, int max_pages, long long ld_table,
+                      int* slots, int max_slots, int* row_start, int* kv_len_out, int* free_end);
+int pafu_paged_slots(void* stream, const int* block_table, int max_pages, long long ld_table, const int* start,
+                     const int* count, int B, int page_size, int* slots, int max_slots, int* row_start);
+
+/* pafu_paged_append - K/V rows to their slots.
+ *   K_pages[slots[t]] = K[t], V_pages[slots[t]] = V[t] for t in [0, rows); with kv_dtype PAFU_FP8_E4M3 the codes that
+ *   pafu_quantize_kv gives.
+ *   K, V : [rows, N, D] bf16, token stride ld_in elements      slots : [rows] int32
+ * A slot outside [0, n_pages * page_size) leaves its row out.  Slots are distinct: of two rows with one slot either may
+ * be kept, 16 bytes at a time.
+ */
+int pafu_paged_append(void* stream, const void* K, const void* V, long long ld_in, int rows, const int* slots, int N,
+                      int D, void* K_pages, void* V_pages, int n_pages, int page_size, long long ld_page,
+                      long long ld_token, long long ld_head, int kv_dtype, int k_scale_log2, int v_scale_log2);
+
+/* pafu_paged_attention - attention of one new token per request over its cached tokens (its own row, appended first,
+ * among them).
+ *   O[b,h,:] = sum_j softmax_j( scale * Q[b,h] . k[j, h / G] ) v[j, h / G]      G = N / N_kv
+ * over the visible tokens j of request b: j < kv_len[b] and, where window > 0, j < n_pinned or j >= kv_len[b] - window
+ * (a sliding window behind a frame sink).  A token on a page outside [0, n_pages) or beyond max_pages is not visible.
+ * A row without a visible token is 0 (as is one whose scores are all -infinity).
+ *   Q : [B, N, D] bf16, stride ld_q      O : [B, N, D] of out_dtype (bf16 or fp32), stride ld_o
+ *   N a multiple of N_kv                 softmax_scale <= 0 means 1/sqrt(D)
+ *   kv_len : [B]                         block_table : [B, max_pages], stride ld_table; 32-bit page numbers, pools of
+ *                                        any size
+ *   workspace : optional (NULL / 0 allowed).  With pafu_paged_attention_workspace_bytes(B, N, N_kv, D) bytes (16-byte
+ *               aligned, apart from every tensor of the call) the tokens of all requests are shared out evenly over the GPU:
+ *               long requests are cut along the token axis and joined in a second pass.  Its contents need not be
+ *               initialised and are not kept.
+ * Products are formed from the bf16 (or widened 8-bit) values exactly and summed in fp32; the softmax weights enter the
+ * second product as the sum of two bf16 numbers (2^-17 off at most), so the result is that of fp32 arithmetic.
+ * Results do not depend on timing; where requests are cut depends on the lengths in the call, which moves the last
+ * bits of an fp32 result.
+ */
+size_t pafu_paged_attention_workspace_bytes(int B, int N, int N_kv, int D);
+int pafu_paged_attention(void* stream, const void* Q, long long ld_q, const void* K_pages, const void* V_pages,
+                         int n_pages, int page_size, long long ld_page, long long ld_token, long long ld_head,
+                         int kv_dtype, int k_scale_log2, int v_scale_log2, const int* block_table, int max_pages,
+                         long long ld_table, const int* kv_len, int B, int N, int N_kv, int D, int n_pinned, int window,
+                         float softmax_scale, void* O, long long ld_o, int out_dtype, void* workspace,
+                         size_t workspace_bytes);
+
+/* ------------------------------------------------------------------------------------------
  * pafu_sse_score - Spatialtemporal-balanced Salience Estimation, the teacher-side score that the Salience
  * Estimation Head is trained to predict (Sec. 3.2, Eq. 4-5).
  *

@@ -28,6 +28,8 @@ SYMBOLS = (
     "pafu_quantize_kv", "pafu_dequantize_kv", "pafu_chunk_attention_fp8",
     "pafu_sse_workspace_bytes", "pafu_sse_score",
     "pafu_step_workspace_bytes", "pafu_step", "pafu_step_layers", "pafu_step_layers_shared",
+    "pafu_paged_tables", "pafu_paged_slots", "pafu_paged_append",
+    "pafu_paged_attention_workspace_bytes", "pafu_paged_attention",
 )
 
 
@@ -133,6 +135,22 @@ def _lib():
                                        c_float, c_void_p, c_void_p, c_size_t]
         lib.pafu_step_layers_shared.restype = c_int
         lib.pafu_step_layers_shared.argtypes = [c_void_p, POINTER(pafu_step_args), c_int, c_int]
+        lib.pafu_paged_tables.restype = c_int
+        lib.pafu_paged_tables.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_void_p, c_int, c_void_p,
+                                          c_int, c_longlong, c_void_p, c_int, c_void_p, c_void_p, c_void_p]
+        lib.pafu_paged_slots.restype = c_int
+        lib.pafu_paged_slots.argtypes = [c_void_p, c_void_p, c_int, c_longlong, c_void_p, c_void_p, c_int, c_int, c_void_p,
+                                         c_int, c_void_p]
+        lib.pafu_paged_append.restype = c_int
+        lib.pafu_paged_append.argtypes = [c_void_p, c_void_p, c_void_p, c_longlong, c_int, c_void_p, c_int, c_int, c_void_p,
+                                          c_void_p, c_int, c_int, c_longlong, c_longlong, c_longlong, c_int, c_int, c_int]
+        lib.pafu_paged_attention_workspace_bytes.restype = c_size_t
+        lib.pafu_paged_attention_workspace_bytes.argtypes = [c_int, c_int, c_int, c_int]
+        lib.pafu_paged_attention.restype = c_int
+        lib.pafu_paged_attention.argtypes = [c_void_p, c_void_p, c_longlong, c_void_p, c_void_p, c_int, c_int, c_longlong,
+                                             c_longlong, c_longlong, c_int, c_int, c_int, c_void_p, c_int, c_longlong,
+                                             c_void_p, c_int, c_int, c_int, c_int, c_int, c_int, c_float, c_void_p,
+                                             c_longlong, c_int, c_void_p, c_size_t]
         _LIB = lib
     return _LIB
 
@@ -416,3 +434,135 @@ def pafu_sse_score(Q, K, block_len, out, workspace, softmax_scale=0.0, stream=No
                                workspace.numel() * workspace.element_size())
     _check(rc, "pafu_sse_score")
     return out
+
+
+# ---- paged K/V cache.  Lengths, tables and slots are read on the device, so what the C side cannot see of them (their
+# type, size and device) is checked here.
+
+def _on_current_device(*tensors):
+    import torch
+    device = tensors[0].get_device()
+    if device < 0:
+        raise ValueError("the tensors must be on the GPU")
+    if device != torch.cuda.current_device():
+        raise ValueError("the tensors are on GPU %d and the current device is %d" % (device, torch.cuda.current_device()))
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("the tensors are on different devices")
+
+
+def _int32_list(name, t, n=None):
+    import torch
+    if t.dtype is not torch.int32:
+        raise TypeError("%s must be int32, not %s" % (name, t.dtype))
+    if t.dim() != 1 or (t.shape[0] > 1 and t.stride(0) != 1) or (n is not None and t.shape[0] != n):
+        raise ValueError("%s must be a contiguous list%s, not %s with strides %s"
+                         % (name, "" if n is None else " of %d" % n, tuple(t.shape), t.stride()))
+    return t.data_ptr()
+
+
+def _block_table(t, n):
+    import torch
+    if t.dtype is not torch.int32:
+        raise TypeError("the block table must be int32, not %s" % t.dtype)
+    if t.dim() != 2 or t.shape[0] != n or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("the block table must be [%d, max_pages] with contiguous rows, not %s with strides %s"
+                         % (n, tuple(t.shape), t.stride()))
+    columns = t.shape[1]
+    return t.data_ptr(), columns, t.stride(0) if n > 1 else max(columns, 1)
+
+
+def _pool_dtype(K_pages, V_pages):
+    """dtype code of a page pool after the checks that need its shape: both tensors alike, elements contiguous."""
+    import torch
+    shape, strides = K_pages.shape, K_pages.stride()
+    if len(shape) != 4 or V_pages.shape != shape or V_pages.stride() != strides or strides[3] != 1:
+        raise ValueError("the page tensors must be [n_pages, page_size, N_kv, D] of one shape and stride, elements contiguous")
+    if V_pages.dtype is not K_pages.dtype or K_pages.dtype not in (torch.bfloat16, torch.uint8):
+        raise TypeError("page tensors are bfloat16 or uint8 (E4M3 codes), not %s and %s" % (K_pages.dtype, V_pages.dtype))
+    return PAFU_BF16 if K_pages.dtype is torch.bfloat16 else PAFU_FP8_E4M3
+
+
+def _rows_3d(name, t, dtypes):
+    """[rows, heads, D] with contiguous rows of one of `dtypes` -> token stride."""
+    if t.dtype not in dtypes:
+        raise TypeError("%s has the unsupported dtype %s" % (name, t.dtype))
+    if t.dim() != 3:
+        raise ValueError("%s must be [rows, heads, D], not %s" % (name, tuple(t.shape)))
+    rows, heads, D = t.shape
+    if (D > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != D):
+        raise ValueError("%s must have contiguous rows, not strides %s" % (name, t.stride()))
+    return t.stride(0) if rows > 1 else heads * D
+
+
+def pafu_paged_tables(kv_len, new_len, free_pages, page_size, block_table, slots, row_start, kv_len_out, free_end,
+                      free_start=None, stream=None):
+    """Pages from free_pages for every request's new tokens, entered in block_table [B, max_pages], and their slots."""
+    B = kv_len.shape[0]
+    _on_current_device(kv_len, new_len, free_pages, block_table, slots, row_start, kv_len_out, free_end, free_start)
+    table, max_pages, ld_table = _block_table(block_table, B)
+    rc = _lib().pafu_paged_tables(_stream(stream), _int32_list("kv_len", kv_len), _int32_list("new_len", new_len, B), B,
+                                  _int32_list("free_pages", free_pages), free_pages.shape[0],
+                                  None if free_start is None else _int32_list("free_start", free_start, 1), page_size,
+                                  table, max_pages, ld_table, _int32_list("slots", slots), slots.shape[0],
+                                  _int32_list("row_start", row_start, B + 1), _int32_list("kv_len_out", kv_len_out, B),
+                                  _int32_list("free_end", free_end, 1))
+    _check(rc, "pafu_paged_tables")
+    return slots
+
+
+def pafu_paged_slots(block_table, start, count, page_size, slots, row_start, stream=None):
+    """Slots of the tokens start[b] .. start[b] + count[b] - 1 of every request, request after request."""
+    B = start.shape[0]
+    _on_current_device(block_table, start, count, slots, row_start)
+    table, max_pages, ld_table = _block_table(block_table, B)
+    rc = _lib().pafu_paged_slots(_stream(stream), table, max_pages, ld_table, _int32_list("start", start),
+                                 _int32_list("count", count, B), B, page_size, _int32_list("slots", slots), slots.shape[0],
+                                 _int32_list("row_start", row_start, B + 1))
+    _check(rc, "pafu_paged_slots")
+    return slots
+
+
+def pafu_paged_append(K, V, slots, K_pages, V_pages, k_scale_log2=0, v_scale_log2=0, stream=None):
+    """K, V: [rows, N, D] bf16 -> K_pages, V_pages: [n_pages, page_size, N, D] bf16, or uint8 E4M3 codes of value /
+    2^scale_log2, at the rows' slots (int32; a slot outside the pool leaves its row out)."""
+    import torch
+    _on_current_device(K, V, slots, K_pages, V_pages)
+    kv_dtype = _pool_dtype(K_pages, V_pages)
+    n_pages, page_size, N, D = K_pages.shape
+    ld_in = _rows_3d("K", K, (torch.bfloat16,))
+    rows = K.shape[0]
+    if K.shape[1] != N or K.shape[2] != D or V.shape != K.shape or _rows_3d("V", V, (torch.bfloat16,)) != ld_in:
+        raise ValueError("K and V must be [rows, %d, %d] with one stride, not %s and %s" % (N, D, tuple(K.shape), tuple(V.shape)))
+    ld = K_pages.stride()
+    rc = _lib().pafu_paged_append(_stream(stream), K.data_ptr(), V.data_ptr(), ld_in, rows, _int32_list("slots", slots, rows),
+                                  N, D, K_pages.data_ptr(), V_pages.data_ptr(), n_pages, page_size, ld[0], ld[1], ld[2],
+                                  kv_dtype, k_scale_log2, v_scale_log2)
+    _check(rc, "pafu_paged_append")
+    return K_pages, V_pages
+
+
+def pafu_paged_attention_workspace_bytes(B: int, N: int, N_kv: int, D: int) -> int:
+    return _lib().pafu_paged_attention_workspace_bytes(B, N, N_kv, D)
+
+
+def pafu_paged_attention(Q, K_pages, V_pages, block_table, kv_len, O, n_pinned=0, window=0, softmax_scale=0.0,
+                         k_scale_log2=0, v_scale_log2=0, workspace=None, stream=None):
+    """Q, O: [B, N, D], one new token per request; K_pages, V_pages: [n_pages, page_size, N_kv, D] bf16 or uint8 codes."""
+    import torch
+    _on_current_device(Q, K_pages, V_pages, block_table, kv_len, O, workspace)
+    kv_dtype = _pool_dtype(K_pages, V_pages)
+    n_pages, page_size, N_kv, D = K_pages.shape
+    ld_q, ld_o = _rows_3d("Q", Q, (torch.bfloat16,)), _rows_3d("O", O, (torch.bfloat16, torch.float32))
+    B, N = Q.shape[0], Q.shape[1]
+    if Q.shape[2] != D or O.shape != Q.shape:
+        raise ValueError("Q and O must be [B, N, %d], not %s and %s" % (D, tuple(Q.shape), tuple(O.shape)))
+    table, max_pages, ld_table = _block_table(block_table, B)
+    ld = K_pages.stride()
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    rc = _lib().pafu_paged_attention(_stream(stream), Q.data_ptr(), ld_q, K_pages.data_ptr(), V_pages.data_ptr(), n_pages,
+                                     page_size, ld[0], ld[1], ld[2], kv_dtype, k_scale_log2, v_scale_log2, table, max_pages,
+                                     ld_table, _int32_list("kv_len", kv_len, B), B, N, N_kv, D, n_pinned, window,
+                                     float(softmax_scale), O.data_ptr(), ld_o, _dtype_code(O), _ptr(workspace), ws_bytes)
+    _check(rc, "pafu_paged_attention")
+    return O

@@ -153,6 +153,59 @@ int check_quant(const void* Kw, const void* Vw, long long ld_w, int rows, int N,
   return PAFU_OK;
 }
 
+// The pool of a paged cache, and its strides as byte strides.  The stride of an axis of length one is not read: it is set
+// to what a dense pool would have.
+int check_pool(const void* K, const void* V, int n_pages, int page_size, long long ld_page, long long ld_token,
+               long long ld_head, int N, int D, int dtype, PagedPool& pool) {
+  if (n_pages < 1 || N < 1 || page_size < 8 || page_size > 4096 || (page_size & (page_size - 1)) != 0) return PAFU_ERR_SHAPE;
+  if (D != 64 && D != 128) return PAFU_ERR_SHAPE;
+  if (dtype != PAFU_BF16 && dtype != PAFU_FP8_E4M3) return PAFU_ERR_DTYPE;
+  const long long eb = kv_dtype_bytes(dtype), most = 1ll << 40;
+  if (N == 1) ld_head = D;
+  if (ld_head < D || ld_token < D || ld_head > most || ld_token > most || N > (1 << 20)) return PAFU_ERR_SHAPE;
+  const bool heads_inside = ld_token >= (N - 1) * ld_head + D, tokens_inside = ld_head >= (page_size - 1) * ld_token + D;
+  if (!heads_inside && !tokens_inside && N > 1) return PAFU_ERR_SHAPE;
+  const long long page = (page_size - 1) * ld_token + (N - 1) * ld_head + D;  // elements from a page's first to its last
+  if (n_pages == 1) ld_page = (page + 15) / 16 * 16;
+  if (ld_page < page || ld_page > most || n_pages - 1 > (1ll << 60) / ld_page) return PAFU_ERR_SHAPE;
+  if (!K || !V) return PAFU_ERR_NULL;
+  if (!aligned16(K) || !aligned16(V) || (ld_page * eb) % 16 != 0 || (ld_token * eb) % 16 != 0 || (ld_head * eb) % 16 != 0)
+    return PAFU_ERR_ALIGN;
+  int log2 = 3;
+  while ((1 << log2) < page_size) ++log2;
+  pool = PagedPool{static_cast<const char*>(K), static_cast<const char*>(V), ld_page * eb, ld_token * eb, ld_head * eb,
+                   n_pages, log2};
+  return PAFU_OK;
+}
+// What a pool's tensor spans: tokens at one stride where the pages follow each other without a gap (K and V may then lie
+// side by side in a token), pages otherwise.
+Span pool_span(const void* p, const PagedPool& pool, int N, int D, int dtype) {
+  const long long page_size = 1ll << pool.page_log2;
+  const long long token = (N - 1) * pool.ld_head + (long long)D * kv_dtype_bytes(dtype);
+  if (pool.ld_page == page_size * pool.ld_token && pool.ld_token >= token)
+    return Span{p, pool.n_pages * page_size, pool.ld_token, token};
+  return Span{p, pool.n_pages, pool.ld_page, (page_size - 1) * pool.ld_token + token};
+}
+// Does any of `outs` overlap another of them or any of `ins`?
+template <int N_OUT, int N_IN>
+bool any_overlap(const Span (&outs)[N_OUT], const Span (&ins)[N_IN]) {
+  for (int i = 0; i < N_OUT; ++i) {
+    for (int j = 0; j < i; ++j)
+      if (spans_overlap(outs[i], outs[j])) return true;
+    for (const Span& in : ins)
+      if (spans_overlap(outs[i], in)) return true;
+  }
+  return false;
+}
+int check_paged_lists(int B, int page_size, int max_pages, long long ld_table, int max_slots, int& page_log2) {
+  if (B < 0 || B > PAFU_PAGED_MAX_REQUESTS || max_pages < 1 || ld_table < max_pages || ld_table > (1ll << 40) || max_slots < 0)
+    return PAFU_ERR_SHAPE;
+  if (page_size < 8 || page_size > 4096 || (page_size & (page_size - 1)) != 0) return PAFU_ERR_SHAPE;
+  page_log2 = 3;
+  while ((1 << page_log2) < page_size) ++page_log2;
+  return PAFU_OK;
+}
+
 // Everything a step reads and everything it writes (the workspace apart).  `scoring` is false for a layer that takes
 // its indices from another layer: then only the cache part counts.
 struct StepSpans {
@@ -798,6 +851,107 @@ int pafu_chunk_attention_gather(void* stream, const void* Q, int Lq, const void*
   const AttnLayer layer{Q, K_cache, V_cache, Kn, Vn, O};
   return launch_attention(static_cast<hipStream_t>(stream), &layer, 1, Lq, n_kept, Lc, N, D, ld_q, ld_c, ld_n, ld_o,
                           block_len, scale, out_dtype, workspace, workspace_bytes, ids, n_cache);
+}
+
+int pafu_paged_tables(void* stream, const int* kv_len, const int* new_len, int B, const int* free_pages, int n_free,
+                      const int* free_start, int page_size, int* block_table, int max_pages, long long ld_table,
+                      int* slots, int max_slots, int* row_start, int* kv_len_out, int* free_end) {
+  PagedTables t{kv_len, new_len, free_pages, free_start, block_table, slots, row_start, kv_len_out, free_end, ld_table,
+                B, n_free, 0, max_pages, max_slots};
+  int rc = check_paged_lists(B, page_size, max_pages, ld_table, max_slots, t.page_log2);
+  if (rc) return rc;
+  if (n_free < 0) return PAFU_ERR_SHAPE;
+  if (B == 0) return PAFU_OK;
+  if (!kv_len || !new_len || (n_free > 0 && !free_pages) || !block_table || (max_slots > 0 && !slots) || !row_start ||
+      !kv_len_out || !free_end)
+    return PAFU_ERR_NULL;
+  if (!aligned16(kv_len) || !aligned16(new_len) || !aligned16(free_pages) || !aligned16(block_table) || !aligned16(slots) ||
+      !aligned16(row_start) || !aligned16(kv_len_out) || (reinterpret_cast<uintptr_t>(free_start) & 3u) != 0 ||
+      (reinterpret_cast<uintptr_t>(free_end) & 3u) != 0)
+    return PAFU_ERR_ALIGN;
+  const Span ins[] = {{kv_len, 1, 0, B * 4ll}, {new_len, 1, 0, B * 4ll}, {free_pages, 1, 0, n_free * 4ll}, {free_start, 1, 0, 4}};
+  const Span outs[] = {{block_table, B, ld_table * 4, max_pages * 4ll}, {slots, 1, 0, max_slots * 4ll},
+                       {row_start, 1, 0, (B + 1) * 4ll}, {kv_len_out, 1, 0, B * 4ll}, {free_end, 1, 0, 4}};
+  if (any_overlap(outs, ins)) return PAFU_ERR_ALIAS;
+  return launch_paged_tables(static_cast<hipStream_t>(stream), t, true);
+}
+
+int pafu_paged_slots(void* stream, const int* block_table, int max_pages, long long ld_table, const int* start,
+                     const int* count, int B, int page_size, int* slots, int max_slots, int* row_start) {
+  // (the table is only read: this launch takes no pages)
+  PagedTables t{start, count, nullptr, nullptr, const_cast<int*>(block_table), slots, row_start, nullptr, nullptr, ld_table,
+                B, 0, 0, max_pages, max_slots};
+  int rc = check_paged_lists(B, page_size, max_pages, ld_table, max_slots, t.page_log2);
+  if (rc) return rc;
+  if (B == 0) return PAFU_OK;
+  if (!block_table || !start || !count || (max_slots > 0 && !slots) || !row_start) return PAFU_ERR_NULL;
+  if (!aligned16(block_table) || !aligned16(start) || !aligned16(count) || !aligned16(slots) || !aligned16(row_start))
+    return PAFU_ERR_ALIGN;
+  const Span ins[] = {{block_table, B, ld_table * 4, max_pages * 4ll}, {start, 1, 0, B * 4ll}, {count, 1, 0, B * 4ll}};
+  const Span outs[] = {{slots, 1, 0, max_slots * 4ll}, {row_start, 1, 0, (B + 1) * 4ll}};
+  if (any_overlap(outs, ins)) return PAFU_ERR_ALIAS;
+  return launch_paged_tables(static_cast<hipStream_t>(stream), t, false);
+}
+
+int pafu_paged_append(void* stream, const void* K, const void* V, long long ld_in, int rows, const int* slots, int N,
+                      int D, void* K_pages, void* V_pages, int n_pages, int page_size, long long ld_page,
+                      long long ld_token, long long ld_head, int kv_dtype, int k_scale_log2, int v_scale_log2) {
+  PagedPool pool;
+  int rc = check_pool(K_pages, V_pages, n_pages, page_size, ld_page, ld_token, ld_head, N, D, kv_dtype, pool);
+  if (rc) return rc;
+  const long long row = (long long)N * D;
+  if (rows < 0 || ld_in < row || ld_in > (1ll << 30) || row > (1 << 24)) return PAFU_ERR_SHAPE;
+  if (!scale_ok(k_scale_log2) || !scale_ok(v_scale_log2)) return PAFU_ERR_SHAPE;
+  if (rows == 0) return PAFU_OK;
+  if (!K || !V || !slots) return PAFU_ERR_NULL;
+  if (!aligned16(K) || !aligned16(V) || !aligned16(slots) || (ld_in * 2) % 16 != 0) return PAFU_ERR_ALIGN;
+  const Span ins[] = {{K, rows, ld_in * 2, row * 2}, {V, rows, ld_in * 2, row * 2}, {slots, 1, 0, rows * 4ll}};
+  const Span outs[] = {pool_span(K_pages, pool, N, D, kv_dtype), pool_span(V_pages, pool, N, D, kv_dtype)};
+  if (any_overlap(outs, ins)) return PAFU_ERR_ALIAS;
+  return launch_paged_append(static_cast<hipStream_t>(stream), K, V, ld_in * 2, rows, slots, N, D, pool, kv_dtype,
+                             k_scale_log2, v_scale_log2);
+}
+
+size_t pafu_paged_attention_workspace_bytes(int B, int N, int N_kv, int D) {
+  if (B < 1 || N < 1 || N_kv < 1 || N % N_kv != 0 || (D != 64 && D != 128)) return 0;
+  return paged_attention_workspace_bytes(B, N, N_kv, D);
+}
+
+int pafu_paged_attention(void* stream, const void* Q, long long ld_q, const void* K_pages, const void* V_pages,
+                         int n_pages, int page_size, long long ld_page, long long ld_token, long long ld_head,
+                         int kv_dtype, int k_scale_log2, int v_scale_log2, const int* block_table, int max_pages,
+                         long long ld_table, const int* kv_len, int B, int N, int N_kv, int D, int n_pinned, int window,
+                         float softmax_scale, void* O, long long ld_o, int out_dtype, void* workspace,
+                         size_t workspace_bytes) {
+  PagedPool pool;
+  int rc = check_pool(K_pages, V_pages, n_pages, page_size, ld_page, ld_token, ld_head, N_kv, D, kv_dtype, pool);
+  if (rc) return rc;
+  int log2;
+  rc = check_paged_lists(B, page_size, max_pages, ld_table, 0, log2);
+  if (rc) return rc;
+  if (N < 1 || N > (1 << 16) || N % N_kv != 0 || n_pinned < 0 || window < 0) return PAFU_ERR_SHAPE;
+  const int ob = dtype_bytes(out_dtype);
+  if (ob == 0) return PAFU_ERR_DTYPE;
+  const long long row = (long long)N * D;
+  if (ld_q < row || ld_o < row || ld_q > (1ll << 30) || ld_o > (1ll << 30)) return PAFU_ERR_SHAPE;
+  if (!scale_ok(k_scale_log2) || !scale_ok(v_scale_log2)) return PAFU_ERR_SHAPE;
+  if (B == 0) return PAFU_OK;
+  if (!Q || !block_table || !kv_len || !O) return PAFU_ERR_NULL;
+  if (!aligned16(Q) || !aligned16(block_table) || !aligned16(kv_len) || !aligned16(O) || (ld_q * 2) % 16 != 0 ||
+      (ld_o * ob) % 16 != 0)
+    return PAFU_ERR_ALIGN;
+  if (workspace != nullptr && workspace_bytes > 0 && !aligned16(workspace)) return PAFU_ERR_ALIGN;
+  const Span ins[] = {{Q, B, ld_q * 2, row * 2}, pool_span(K_pages, pool, N_kv, D, kv_dtype),
+                      pool_span(V_pages, pool, N_kv, D, kv_dtype), {block_table, B, ld_table * 4, max_pages * 4ll},
+                      {kv_len, 1, 0, B * 4ll}};
+  const Span outs[] = {{O, B, ld_o * ob, row * ob}, {workspace, 1, 0, (long long)workspace_bytes}};
+  if (any_overlap(outs, ins)) return PAFU_ERR_ALIAS;
+  const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)D);
+  const bool kv8 = kv_dtype == PAFU_FP8_E4M3;
+  const PagedAttention a{Q, O, block_table, kv_len, ld_q * 2, ld_o * ob, ld_table, B, N, N_kv, D, max_pages, n_pinned, window,
+                         kv_dtype, out_dtype, scale, kv8 ? ldexpf(1.0f, k_scale_log2) : 1.0f,
+                         kv8 ? ldexpf(1.0f, v_scale_log2) : 1.0f};
+  return launch_paged_attention(static_cast<hipStream_t>(stream), a, pool, workspace, workspace_bytes);
 }
 
 size_t pafu_sse_workspace_bytes(int L, int N) { return L > 0 && N > 0 ? sse_workspace_bytes(L, N) : 0; }

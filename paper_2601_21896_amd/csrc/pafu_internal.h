@@ -141,6 +141,35 @@ int launch_quantize(hipStream_t st, const void* K, const void* V, long long ld_i
                     int k_scale_log2, int v_scale_log2, void* Kq, void* Vq, long long ld_out_bytes);
 int launch_dequantize(hipStream_t st, const void* Kq, const void* Vq, long long ld_in_bytes, int rows, int row_elems,
                       int k_scale_log2, int v_scale_log2, void* K, void* V, long long ld_out_bytes);
+// Paged K/V cache.  The pool's strides in bytes.
+struct PagedPool {
+  const char* K;
+  const char* V;
+  long long ld_page, ld_token, ld_head;
+  int n_pages, page_log2;
+};
+// Block tables and slots.  free_pages null: slots only, of tokens start .. start + count - 1 that have their pages.
+struct PagedTables {
+  const int *start, *count, *free_pages, *free_start;
+  int* table;
+  int *slots, *row_start, *kv_len_out, *free_end;
+  long long ld_table;
+  int B, n_free, page_log2, max_pages, max_slots;
+};
+int launch_paged_tables(hipStream_t st, const PagedTables& t, bool take_pages);
+int launch_paged_append(hipStream_t st, const void* K, const void* V, long long ld_in_bytes, int rows, const int* slots,
+                        int N, int D, const PagedPool& pool, int kv_dtype, int k_scale_log2, int v_scale_log2);
+struct PagedAttention {
+  const void* Q;
+  void* O;
+  const int *table, *kv_len;
+  long long ld_q, ld_o, ld_table;  // ld_q, ld_o in bytes
+  int B, N, N_kv, D, max_pages, n_pinned, window, kv_dtype, out_dtype;
+  float scale, k_scale, v_scale;
+};
+size_t paged_attention_workspace_bytes(int B, int N, int N_kv, int D);
+int launch_paged_attention(hipStream_t st, const PagedAttention& a, const PagedPool& pool, void* workspace,
+                           size_t workspace_bytes);
 // Compute units of the current GPU (cached per device; 256 if the query fails).
 int compute_units();
 
