@@ -929,7 +929,9 @@ int pafu_paged_attention(void* stream, const void* Q, long long ld_q, const void
   int log2;
   rc = check_paged_lists(B, page_size, max_pages, ld_table, 0, log2);
   if (rc) return rc;
-  if (N < 1 || N > (1 << 16) || N % N_kv != 0 || n_pinned < 0 || window < 0) return PAFU_ERR_SHAPE;
+  if (N < 1 || N > (1 << 16) - 1 || N % N_kv != 0 || n_pinned < 0 || window < 0) return PAFU_ERR_SHAPE;
+  // the tiles of all requests are counted in 32 bits
+  if (B > 0 && ((((long long)max_pages << pool.page_log2) + 31) / 32) > 0x7fffffffll / B) return PAFU_ERR_SHAPE;
   const int ob = dtype_bytes(out_dtype);
   if (ob == 0) return PAFU_ERR_DTYPE;
   const long long row = (long long)N * D;
