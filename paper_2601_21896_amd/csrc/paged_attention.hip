@@ -3,8 +3,7 @@
 //
 //   O[b,h] = sum_j w_j v[j] / sum_j w_j,   w_j = 2^(s_j - m),   s_j = scale * log2(e) * q[b,h] . k[j]
 //
-// The tokens of a request are taken in tiles of 32.  A wave works alone: no LDS, no barrier.  For a tile it forms
-// S^T = K Q^T (16 query heads of the group as columns), the weights, and O^T += V^T W^T, all on 16x16x32 matrix
+// The tokens of a request are taken in tiles of 32, a wave works on a tile alone.  It forms S^T = K Q^T (16 query heads of the group as columns), the weights, and O^T += V^T W^T, all on 16x16x32 matrix
 // instructions.  The rows of the two S^T blocks of a tile are dealt to tokens so that a lane's eight weights are those
 // of eight neighbouring tokens, 8 g .. 8 g + 7 for lane group g, which is the operand layout of the second product: the
 // weights never leave their lane.  V is read by rows, a lane its 8 (or 4) neighbouring elements of its group's eight
@@ -29,19 +28,22 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoMax = -3.0e38f;   // softmax reference before the first visible token
 constexpr float kRaiseAt = 8.f;      // weights up to 2^8: the reference is raised when a score passes it by more
 constexpr int kTile = 32;            // tokens
-constexpr int kWaves = 4;            // per workgroup; they share nothing but the launch
-constexpr int kMinShare = 4;         // tiles that a wave takes at least where requests are cut
+constexpr int kWaves = 4;           // per workgroup
+constexpr int kMinShare = 4;         // tiles of a column at least where requests are cut
+constexpr int kLong = 16;            // tiles from which a request is worth a workgroup
 
-// How the work is laid out.  A column is a run of tiles of the requests' concatenated tile lists; every (key head, group of
-// query heads) of a column is one wave, and these are neighbours in the launch: they read neighbouring memory.
+// How the work is laid out.  A column is a run of tiles of the requests' concatenated tile lists, or, where nothing is cut, a
+// request.  Every (key head, group of query heads) of a column is one wave, neighbouring heads are one workgroup
+// ("narrow"), or it is a workgroup, whose waves take the tiles in turn and add up in LDS ("wide").
 struct Layout {
-  int columns;     // cut: runs of equal length; whole: one per request
-  int heads;       // waves per column = N_kv * groups
+  int columns;
+  int heads;       // waves or workgroups per column = N_kv * groups
   int groups;      // of 16 * QT query heads that share a key head
   int cut;
+  int joined;      // the requests, or, where they are more than the columns, the columns that a request may go on from
   float* partial;  // [columns][2][N][D]: 0 = the request began in an earlier column, 1 = it goes on in the next one
   float2* stat;    // [columns][2][N]: softmax reference and sum of a partial result
-  int2* joins;     // [columns]: request that begins in the column and goes on, number of columns it spans (0: none)
+  int2* joins;     // [joined]: first column and number of columns of a request that is cut (0 columns: it is not)
 };
 
 // The tiles of a request.  Visible are [0, pin) and [lo, len).
@@ -69,17 +71,14 @@ __device__ __forceinline__ Tiles request_tiles(const PagedAttention& a, int page
   return t;
 }
 
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
-  return x;
-}
-__device__ __forceinline__ int wave_scan(int x, int lane) {  // inclusive
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
+// inclusive sums over the wave's lanes
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1, 2, 4, 8: within 16 lanes
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
   return x;
 }
 
@@ -92,18 +91,23 @@ struct Raw {
   unsigned v[8][kVWords];
 };
 
-template <int WORDS>
+template <bool ONCE, typename T>
+__device__ __forceinline__ T load(const char* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const T*>(p));
+  return *reinterpret_cast<const T*>(p);
+}
+template <bool ONCE, int WORDS>
 __device__ __forceinline__ void load_words(const char* p, unsigned (&w)[WORDS]) {
   if constexpr (WORDS == 4) {
-    const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+    const u32x4 x = load<ONCE, u32x4>(p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = x[i];
   } else if constexpr (WORDS == 2) {
-    const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+    const u32x2 x = load<ONCE, u32x2>(p);
     w[0] = x[0];
     w[1] = x[1];
   } else {
-    w[0] = *reinterpret_cast<const unsigned*>(p);
+    w[0] = load<ONCE, unsigned>(p);
   }
 }
 
@@ -113,62 +117,79 @@ __device__ __forceinline__ unsigned widen2(unsigned w, bool upper) {
                : __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
 }
 
-template <int D, bool KV8, int QT, bool OUT_F32>
-__global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(PagedAttention a, PagedPool pool, Layout ly) {
+template <int D, bool KV8, int QT, bool WIDE>
+__global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAttention a, PagedPool pool, Layout ly) {
   constexpr int kSteps = D / 32;   // matrix instructions of one S^T block
   constexpr int kBlocks = D / 16;  // blocks of O^T
+  constexpr bool kOnce = QT == 1;  // K and V are read by one wave only
   using R = Raw<D, KV8>;
+  constexpr int kWays = WIDE ? kWaves : 1;
+  __shared__ f32x4 part[kWays][QT][4][kBlocks / 4][WIDE ? 64 : 1];
+  __shared__ float2 part_stat[kWays][QT][16];
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
-  const int id = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + (threadIdx.x >> 6));
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int G = a.N / a.N_kv, out_bytes = a.out_dtype == PAFU_F32 ? 4 : 2;
+
+  // ---- the tiles of all requests
+  int total = 0, mine = 0, ends = 0;  // mine, ends: of request `lane`, the last ones summed
+  if (ly.cut) {
+    for (int r0 = 0; r0 < a.B; r0 += 64) {
+      const int r = r0 + lane;
+      mine = r < a.B ? request_tiles(a, pool.page_log2, a.kv_len[r]).n : 0;
+      ends = total + wave_scan(mine);
+      total = __builtin_amdgcn_readlane(ends, 63);
+    }
+  }
+  const int columns = ly.columns, sub = WIDE ? wave : 0;
+  const int id = WIDE ? blockIdx.x : blockIdx.x * kWaves + wave;
   const int x = id / ly.heads, head_id = id - x * ly.heads;
-  if (x >= ly.columns) return;
+  if (x >= columns) return;
   const int kvh = head_id / ly.groups, group = head_id - kvh * ly.groups;
-  const int G = a.N / a.N_kv;
 
   // ---- this column's tiles: request b from its tile `at` on, `left` tiles
-  int b = 0, at = 0, left = 0, share = 0, before = 0;  // before: tiles of the requests in front of b
+  int b = x, at = 0, left = 0x7fffffff, share = 0, before = 0;  // before: tiles of the requests in front of b
   if (ly.cut) {
-    int mine = 0;
-    for (int r = lane; r < a.B; r += 64) mine += request_tiles(a, pool.page_log2, a.kv_len[r]).n;
-    const int total = wave_sum(mine);
-    share = (total + ly.columns - 1) / ly.columns;
-    if (share < kMinShare) share = kMinShare;
+    share = (total + columns - 1) / columns;
+    if (WIDE && share < kWays) share = kWays;
+    left = 0;
     const long long first = (long long)x * share;
     if (first < total) {
       left = min(share, total - (int)first);
-      for (int r0 = 0; r0 < a.B; r0 += 64) {
-        const int r = r0 + lane, t = r < a.B ? request_tiles(a, pool.page_log2, a.kv_len[r]).n : 0;
-        const int ends = before + wave_scan(t, lane);
+      for (int r0 = 0;; r0 += 64) {
+        if (a.B > 64) {
+          const int r = r0 + lane;
+          mine = r < a.B ? request_tiles(a, pool.page_log2, a.kv_len[r]).n : 0;
+          ends = before + wave_scan(mine);
+        }
         const unsigned long long beyond = __ballot(ends > (int)first);
         if (beyond) {
           const int l = __ffsll(beyond) - 1;
-          b = __builtin_amdgcn_readfirstlane(r0 + l);
-          before = __builtin_amdgcn_readfirstlane(__shfl(ends - t, l));
+          b = r0 + l;
+          before = __builtin_amdgcn_readlane(ends - mine, l);
           at = (int)first - before;
           break;
         }
-        before = __builtin_amdgcn_readfirstlane(__shfl(ends, 63));
+        before = __builtin_amdgcn_readlane(ends, 63);
       }
     }
-  } else {
-    b = x;
-    left = 0x7fffffff;
   }
-  left = __builtin_amdgcn_readfirstlane(left);
 
+  // joins are told by request, or by column with the request in the first place
+  const bool by_request = ly.cut && ly.joined == a.B, tells = ly.cut && head_id == 0 && sub == 0 && lane == 0;
   // ---- requests without tiles
-  for (int r = x; r < a.B; r += ly.columns) {
-    const int kv_len = __builtin_amdgcn_readfirstlane(a.kv_len[r]);
-    if (request_tiles(a, pool.page_log2, kv_len).n > 0) continue;
+  for (int r = x; r < a.B; r += columns) {
+    if (request_tiles(a, pool.page_log2, a.kv_len[r]).n > 0) continue;
     const int h0 = kvh * G + group * 16 * QT, rows = min(16 * QT, G - group * 16 * QT);
-    char* to = static_cast<char*>(a.O) + r * a.ld_o + (long long)h0 * D * (OUT_F32 ? 4 : 2);
-    for (int i = lane; i < rows * D * (OUT_F32 ? 4 : 2) / 16; i += 64) reinterpret_cast<u32x4*>(to)[i] = u32x4{0, 0, 0, 0};
+    char* to = static_cast<char*>(a.O) + r * a.ld_o + (long long)h0 * D * out_bytes;
+    if (sub == 0)
+      for (int i = lane; i < rows * D * out_bytes / 16; i += 64) reinterpret_cast<u32x4*>(to)[i] = u32x4{0, 0, 0, 0};
+    if (by_request && tells) ly.joins[r] = make_int2(0, 0);
   }
 
   const float sc = a.scale * a.k_scale * kLog2e;
-  int2 join = make_int2(0, 0);
+  int2 join = make_int2(0, 0);  // of the column
   while (left > 0 && b < a.B) {
-    const Tiles t = request_tiles(a, pool.page_log2, __builtin_amdgcn_readfirstlane(a.kv_len[b]));
+    const Tiles t = request_tiles(a, pool.page_log2, a.kv_len[b]);
     const int here = min(t.n - at, left);
     if (here <= 0) {  // no tiles
       if (!ly.cut) break;
@@ -213,28 +234,39 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(PagedAtten
       page = max(min(page, pool.n_pages - 1), 0);
       return page * pool.ld_page + (token & mask) * pool.ld_token;
     };
-    auto load_k = [&](R& raw, int base, int page) {
-      const char* p = Kl + offset(page, base + kgroup * 8);
+    // Where a wave's next tile lies; behind its last one the first row of the pool, one line for all lanes: loads on every path,
+    // in one order, let the compiler wait for just the ones it needs.
+    auto k_at = [&](int base, int page, bool there) { return there ? Kl + offset(page, base + kgroup * 8) : pool.K; };
+    auto v_at = [&](int base, int page, bool there) { return there ? Vl + offset(page, base + g * 8) : pool.V; };
+    auto load_k = [&](R& raw, const char* p) {
 #pragma unroll
       for (int tk = 0; tk < 2; ++tk)
 #pragma unroll
-        for (int i = 0; i < R::kK; ++i) raw.k[tk][i] = *reinterpret_cast<const u32x4*>(p + tk * 4 * pool.ld_token + i * 64);
+        for (int i = 0; i < R::kK; ++i) raw.k[tk][i] = load<kOnce, u32x4>(p + tk * 4 * pool.ld_token + i * 64);
     };
-    auto load_v = [&](R& raw, int base, int page) {
-      const char* p = Vl + offset(page, base + g * 8);
+    auto load_v = [&](R& raw, const char* p) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) load_words(p + j * pool.ld_token, raw.v[j]);
+      for (int j = 0; j < 8; ++j) load_words<kOnce>(p + j * pool.ld_token, raw.v[j]);
     };
+    auto nth = [&](int i) { return tile_base(at + min(i, here - 1)); };
 
+    // Pages are asked for two tiles ahead, K and V one, always in the order K, pages, V: the wait for K then leaves V in flight.
+    auto in_pool = [&](int page) { return page >= 0 && page < pool.n_pages; };
     R raw;
-    int base = tile_base(at);
+    int base = nth(sub), base1 = nth(sub + kWays);
     int page_v = page_at(base + g * 8), page_k = page_at(base + kgroup * 8);
-    load_k(raw, base, page_k);
-    load_v(raw, base, page_v);
-    int next_base = here > 1 ? tile_base(at + 1) : base;
-    int next_v = page_at(next_base + g * 8), next_k = page_at(next_base + kgroup * 8);
+    bool page_ok = in_pool(page_v);
+    const char *k_next = k_at(base, page_k, sub < here), *v_next = v_at(base, page_v, sub < here);
+    page_v = page_at(base1 + g * 8);
+    page_k = page_at(base1 + kgroup * 8);
+    __builtin_amdgcn_sched_barrier(0);
+    load_k(raw, k_next);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(raw, v_next);
+    __builtin_amdgcn_sched_barrier(0);
 
-    for (int i = 0; i < here; ++i) {
+    for (int i = sub; i < here; i += kWays) {
+      const bool more = i + kWays < here;
       // ---- S^T = K Q^T
       f32x4 s[QT][2];
 #pragma unroll
@@ -259,12 +291,17 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(PagedAtten
             s[qt][tk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[e], q[qt][e], s[qt][tk], 0, 0, 0);
         }
       }
-      if (i + 1 < here) load_k(raw, next_base, next_k);
+      k_next = k_at(base1, page_k, more);
+      v_next = v_at(base1, page_v, more);
+      const bool next_ok = in_pool(page_v);
+      const int base2 = nth(i + 2 * kWays);
+      load_k(raw, k_next);
+      page_v = page_at(base2 + g * 8);
+      page_k = page_at(base2 + kgroup * 8);
 
       // ---- what is not visible: s(tk, r) belongs to token base + 8 g + 4 tk + r, V's row j to base + 8 g + j
       const bool pinned = at + i < t.n_pin;
       const int lo = pinned ? 0 : t.lo, hi = pinned ? t.pin : t.len;
-      const bool page_ok = page_v >= 0 && page_v < pool.n_pages;
       if (base < lo || hi - base < kTile || __ballot(!page_ok)) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -330,113 +367,173 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(PagedAtten
           o[qt][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, lo_w[qt], o[qt][k], 0, 0, 0);
         }
       }
-      if (i + 1 < here) {
-        load_v(raw, next_base, next_v);
-        base = next_base;
-        page_v = next_v;
-        next_base = tile_base(min(at + i + 2, at + here - 1));
-        next_v = page_at(next_base + g * 8);
-        next_k = page_at(next_base + kgroup * 8);
-      }
+      load_v(raw, v_next);
+      base = base1;
+      base1 = base2;
+      page_ok = next_ok;
     }
 
-    // ---- out: lane (g, n) holds query n's elements (4 g + r) * kBlocks + k
-    const bool whole = at == 0 && here == t.n;
-    const long long slot = 2ll * x + (at == 0 ? 1 : 0);
+    // ---- out: lane (g, n) holds query n's elements (4 g + r) * kBlocks + k.  The waves of a wide workgroup leave what they
+    // have in LDS, and wave r adds up the elements of its r.
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
       l[qt] += __shfl_xor(l[qt], 16);
       l[qt] += __shfl_xor(l[qt], 32);
-      const int hq = group * 16 * QT + qt * 16 + n;
-      if (hq >= G) continue;
-      const long long h = (long long)kvh * G + hq;
-      if (whole) {
-        const float inv = l[qt] == 0.f ? 0.f : a.v_scale / l[qt];
-        char* to = static_cast<char*>(a.O) + b * a.ld_o + h * D * (OUT_F32 ? 4 : 2);
+    }
+    const bool whole = at == 0 && here == t.n;
+    const long long slot = 2ll * x + (at == 0 ? 1 : 0);
+    if constexpr (WIDE) {
+      __syncthreads();  // the sums of the piece before are formed
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int d = (g * 4 + r) * kBlocks;
-          if constexpr (OUT_F32) {
-#pragma unroll
-            for (int k = 0; k < kBlocks; k += 4)
-              *reinterpret_cast<f32x4*>(to + (d + k) * 4) =
-                  f32x4{o[qt][k][r] * inv, o[qt][k + 1][r] * inv, o[qt][k + 2][r] * inv, o[qt][k + 3][r] * inv};
-          } else {
-            unsigned w[kBlocks / 2];
-#pragma unroll
-            for (int k = 0; k < kBlocks; k += 2) {
-              bf16x2 y;
-              y[0] = (__bf16)(o[qt][k][r] * inv);
-              y[1] = (__bf16)(o[qt][k + 1][r] * inv);
-              w[k >> 1] = __builtin_bit_cast(unsigned, y);
-            }
-            if constexpr (kBlocks == 8) *reinterpret_cast<u32x4*>(to + d * 2) = u32x4{w[0], w[1], w[2], w[3]};
-            else *reinterpret_cast<u32x2*>(to + d * 2) = u32x2{w[0], w[1]};
-          }
-        }
-      } else {
-        float* to = ly.partial + (slot * a.N + h) * D;
+      for (int qt = 0; qt < QT; ++qt) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
           for (int k = 0; k < kBlocks; k += 4)
-            *reinterpret_cast<f32x4*>(to + (g * 4 + r) * kBlocks + k) =
-                f32x4{o[qt][k][r], o[qt][k + 1][r], o[qt][k + 2][r], o[qt][k + 3][r]};
-        if (g == 0) ly.stat[slot * a.N + h] = make_float2(m[qt], l[qt]);
+            part[wave][qt][r][k >> 2][lane] = f32x4{o[qt][k][r], o[qt][k + 1][r], o[qt][k + 2][r], o[qt][k + 3][r]};
+        if (g == 0) part_stat[wave][qt][n] = make_float2(m[qt], l[qt]);
       }
+      __syncthreads();
     }
-    if (at == 0 && here < t.n) join = make_int2(b, (before + t.n - 1) / share - x + 1);
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      const int hq = group * 16 * QT + qt * 16 + n;
+      const long long h = (long long)kvh * G + hq;
+      float top = m[qt], sum = l[qt];
+      float weight[kWays];
+      if constexpr (WIDE) {
+        top = kNoMax;
+        sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWays; ++w) top = fmaxf(top, part_stat[w][qt][n].x);
+#pragma unroll
+        for (int w = 0; w < kWays; ++w) {
+          weight[w] = __builtin_amdgcn_exp2f(part_stat[w][qt][n].x - top);
+          sum += part_stat[w][qt][n].y * weight[w];
+        }
+      }
+      if (hq >= G) continue;
+      const float inv = !whole ? 1.f : (sum == 0.f ? 0.f : a.v_scale / sum);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        f32x4 y[kBlocks / 4];
+        int elements = (g * 4 + r) * kBlocks;
+        if constexpr (WIDE) {
+          if (r > 0) break;  // (this wave's r is its number)
+          elements = (g * 4 + wave) * kBlocks;
+#pragma unroll
+          for (int k = 0; k < kBlocks / 4; ++k) {
+            y[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < kWays; ++w) y[k] += part[w][qt][wave][k][lane] * weight[w];
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < kBlocks / 4; ++k)
+            y[k] = f32x4{o[qt][4 * k][r], o[qt][4 * k + 1][r], o[qt][4 * k + 2][r], o[qt][4 * k + 3][r]};
+        }
+#pragma unroll
+        for (int k = 0; k < kBlocks / 4; ++k) y[k] *= inv;
+        if (!whole || out_bytes == 4) {
+          char* to = whole ? static_cast<char*>(a.O) + b * a.ld_o + (h * D + elements) * 4
+                           : reinterpret_cast<char*>(ly.partial + (slot * a.N + h) * D + elements);
+#pragma unroll
+          for (int k = 0; k < kBlocks / 4; ++k) reinterpret_cast<f32x4*>(to)[k] = y[k];
+        } else {
+          char* to = static_cast<char*>(a.O) + b * a.ld_o + (h * D + elements) * 2;
+          unsigned w[kBlocks / 2];
+#pragma unroll
+          for (int k = 0; k < kBlocks; k += 2) {
+            bf16x2 pair;
+            pair[0] = (__bf16)y[k >> 2][k & 3];
+            pair[1] = (__bf16)y[k >> 2][(k & 3) + 1];
+            w[k >> 1] = __builtin_bit_cast(unsigned, pair);
+          }
+          if constexpr (kBlocks == 8) *reinterpret_cast<u32x4*>(to) = u32x4{w[0], w[1], w[2], w[3]};
+          else *reinterpret_cast<u32x2*>(to) = u32x2{w[0], w[1]};
+        }
+      }
+      if (!whole && g == 0 && sub == 0) ly.stat[slot * a.N + h] = make_float2(top, sum);
+    }
     if (!ly.cut) break;
+    if (at == 0) {
+      const int spans = here < t.n ? (before + t.n - 1) / share - x + 1 : 0;
+      if (spans) join = make_int2(b, spans);
+      if (by_request && tells) ly.joins[b] = make_int2(x, spans);
+    }
     left -= here;
     before += t.n;
     ++b;
     at = 0;
   }
-  if (ly.cut && head_id == 0 && lane == 0) ly.joins[x] = join;
+  if (tells && !by_request) ly.joins[x] = join;
 }
 
-// Joins the partial results of the request that begins in a column and ends in a later one: one workgroup per (column,
-// query head), D / 4 lanes to a partial result, the others take further ones, in a fixed order.
-template <int D, bool OUT_F32>
+// Joins the partial results of a request that is cut: one workgroup per (request, query head), D / 4 lanes to a partial
+// result, four of them asked for at once, the others' in a fixed order.
+template <int D, bool OUT_F32, int SPLIT>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttention a, Layout ly) {
-  constexpr int kLanes = D / 4, kSets = 256 / kLanes;
-  const int x = blockIdx.x, h = blockIdx.y;
-  const int2 join = ly.joins[x];
+  constexpr int kLanes = D / 4 / SPLIT, kSets = 256 / kLanes, kAhead = 4;
+  const int h = blockIdx.y, first = blockIdx.z * (D / SPLIT);  // first element
+  const int2 join = ly.joins[blockIdx.x];
   if (join.y == 0) return;
+  const bool by_request = ly.joined == a.B;
+  const int x = by_request ? join.x : blockIdx.x, b = by_request ? blockIdx.x : join.x;
   __shared__ float sm[kSets], sl[kSets];
   __shared__ f32x4 so[kSets][kLanes];
   const int set = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
   float m = kNoMax, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int p = set; p < join.y; p += kSets) {
-    const long long at = (2ll * (x + p) + (p == 0 ? 1 : 0)) * a.N + h;
-    const float2 st = ly.stat[at];
-    const f32x4 part = *reinterpret_cast<const f32x4*>(ly.partial + at * D + lane * 4);
-    const float up = fmaxf(m, st.x), keep = __builtin_amdgcn_exp2f(m - up), add = __builtin_amdgcn_exp2f(st.x - up);
+  for (int p0 = set; p0 < join.y; p0 += kSets * kAhead) {
+    float2 st[kAhead];
+    f32x4 part[kAhead];
+    float up = m;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int p = p0 + i * kSets;
+      st[i] = make_float2(kNoMax, 0.f);
+      part[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (p < join.y) {
+        const long long at = (2ll * (x + p) + (p == 0 ? 1 : 0)) * a.N + h;
+        st[i] = ly.stat[at];
+        part[i] = *reinterpret_cast<const f32x4*>(ly.partial + at * D + first + lane * 4);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) up = fmaxf(up, st[i].x);
+    const float keep = __builtin_amdgcn_exp2f(m - up);
     m = up;
-    l = l * keep + st.y * add;
-    o = o * keep + part * add;
+    l *= keep;
+    o *= keep;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const float w = __builtin_amdgcn_exp2f(st[i].x - up);
+      l += st[i].y * w;
+      o += part[i] * w;
+    }
   }
-  if (lane == 0) {
-    sm[set] = m;
-    sl[set] = l;
+  const int sets = min(join.y, kSets);
+  if (set < sets) {
+    if (lane == 0) {
+      sm[set] = m;
+      sl[set] = l;
+    }
+    so[set][lane] = o;
   }
-  so[set][lane] = o;
   __syncthreads();
   if (set > 0) return;
-  float up = kNoMax;
-#pragma unroll
-  for (int i = 0; i < kSets; ++i) up = fmaxf(up, sm[i]);
-  l = 0.f;
-  o = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < kSets; ++i) {
+  float up = m;
+  for (int i = 1; i < sets; ++i) up = fmaxf(up, sm[i]);
+  const float keep = __builtin_amdgcn_exp2f(m - up);
+  l *= keep;
+  o *= keep;
+  for (int i = 1; i < sets; ++i) {
     const float w = __builtin_amdgcn_exp2f(sm[i] - up);
     l += sl[i] * w;
     o += so[i][lane] * w;
   }
   o *= l == 0.f ? 0.f : a.v_scale / l;
-  char* to = static_cast<char*>(a.O) + join.x * a.ld_o + ((long long)h * D + lane * 4) * (OUT_F32 ? 4 : 2);
+  char* to = static_cast<char*>(a.O) + b * a.ld_o + ((long long)h * D + first + lane * 4) * (OUT_F32 ? 4 : 2);
   if constexpr (OUT_F32) {
     *reinterpret_cast<f32x4*>(to) = o;
   } else {
@@ -454,59 +551,67 @@ int head_waves(int N, int N_kv) {
   const int G = N / N_kv, rows = 16 * query_tiles(G);
   return N_kv * ((G + rows - 1) / rows);
 }
-// Columns of a cut launch: 12 waves per compute unit.
-int cut_columns(int N, int N_kv) {
-  const int columns = 12 * compute_units() / head_waves(N, N_kv);
+// Columns of a cut launch: eight waves per compute unit, which are all there at once.
+int cut_columns(int N, int N_kv, bool wide) {
+  const int columns = 8 * compute_units() / (wide ? kWaves : 1) / head_waves(N, N_kv);
   return columns < 1 ? 1 : columns;
 }
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
-template <int D, bool KV8>
-int launch(hipStream_t st, const PagedAttention& a, const PagedPool& pool, const Layout& ly) {
-  const unsigned blocks = (unsigned)(((long long)ly.columns * ly.heads + kWaves - 1) / kWaves);
-  const dim3 threads(64 * kWaves);
-  const bool f32 = a.out_dtype == PAFU_F32;
-  if (query_tiles(a.N / a.N_kv) == 1) {
-    if (f32) hipLaunchKernelGGL((paged_attention_kernel<D, KV8, 1, true>), dim3(blocks), threads, 0, st, a, pool, ly);
-    else hipLaunchKernelGGL((paged_attention_kernel<D, KV8, 1, false>), dim3(blocks), threads, 0, st, a, pool, ly);
-  } else {
-    if (f32) hipLaunchKernelGGL((paged_attention_kernel<D, KV8, 2, true>), dim3(blocks), threads, 0, st, a, pool, ly);
-    else hipLaunchKernelGGL((paged_attention_kernel<D, KV8, 2, false>), dim3(blocks), threads, 0, st, a, pool, ly);
-  }
+template <int D, int SPLIT>
+void launch_join(hipStream_t st, const PagedAttention& a, const Layout& ly) {
+  const dim3 grid((unsigned)ly.joined, (unsigned)a.N, SPLIT);
+  if (a.out_dtype == PAFU_F32) hipLaunchKernelGGL((paged_join_kernel<D, true, SPLIT>), grid, dim3(256), 0, st, a, ly);
+  else hipLaunchKernelGGL((paged_join_kernel<D, false, SPLIT>), grid, dim3(256), 0, st, a, ly);
+}
+template <int D, bool KV8, int QT>
+int launch(hipStream_t st, const PagedAttention& a, const PagedPool& pool, const Layout& ly, bool wide) {
+  const long long jobs = (long long)ly.columns * ly.heads;
+  const dim3 threads(64 * kWaves), blocks((unsigned)(wide ? jobs : (jobs + kWaves - 1) / kWaves));
+  if (wide) hipLaunchKernelGGL((paged_attention_kernel<D, KV8, QT, true>), blocks, threads, 0, st, a, pool, ly);
+  else hipLaunchKernelGGL((paged_attention_kernel<D, KV8, QT, false>), blocks, threads, 0, st, a, pool, ly);
   int rc = check_launch();
   if (rc || !ly.cut) return rc;
-  const dim3 grid((unsigned)ly.columns, (unsigned)a.N);
-  if (f32) hipLaunchKernelGGL((paged_join_kernel<D, true>), grid, dim3(256), 0, st, a, ly);
-  else hipLaunchKernelGGL((paged_join_kernel<D, false>), grid, dim3(256), 0, st, a, ly);
+  // few requests in many columns: four workgroups to a row, which ask for four times as many partial results at once
+  if (ly.columns >= 128 * ly.joined) launch_join<D, 4>(st, a, ly);
+  else launch_join<D, 1>(st, a, ly);
   return check_launch();
+}
+template <int D, bool KV8>
+int launch(hipStream_t st, const PagedAttention& a, const PagedPool& pool, const Layout& ly, bool wide) {
+  return query_tiles(a.N / a.N_kv) == 1 ? launch<D, KV8, 1>(st, a, pool, ly, wide) : launch<D, KV8, 2>(st, a, pool, ly, wide);
 }
 
 }  // namespace
 
 size_t paged_attention_workspace_bytes(int B, int N, int N_kv, int D) {
   (void)B;
-  const size_t columns = (size_t)cut_columns(N, N_kv), rows = columns * 2 * N;
+  const size_t columns = (size_t)cut_columns(N, N_kv, false), rows = columns * 2 * N;
   return rows * D * 4 + round16(rows * 8) + round16(columns * 8);
 }
 
 int launch_paged_attention(hipStream_t st, const PagedAttention& a, const PagedPool& pool, void* workspace,
                            size_t workspace_bytes) {
   Layout ly;
-  const int G = a.N / a.N_kv;
   ly.heads = head_waves(a.N, a.N_kv);
   ly.groups = ly.heads / a.N_kv;
-  (void)G;
   const long long longest = ((((long long)a.max_pages << pool.page_log2) + kTile - 1) / kTile);
   ly.cut = workspace != nullptr && workspace_bytes >= paged_attention_workspace_bytes(a.B, a.N, a.N_kv, a.D) &&
            longest > kMinShare;
   ly.columns = a.B;
+  ly.joined = 0;
   ly.partial = nullptr;
   ly.stat = nullptr;
   ly.joins = nullptr;
+  // Cut: wide where a workgroup's four heads would not be neighbours in memory.  Whole: wide where the requests may be long, or
+  // where the launch has few waves.
+  const bool wide = ly.cut ? ly.heads < kWaves || pool.ld_head > pool.ld_token
+                           : longest >= kLong || (long long)a.B * ly.heads <= 2ll * compute_units();
   if (ly.cut) {
-    const size_t all = (size_t)cut_columns(a.N, a.N_kv);
-    const long long useful = (longest * a.B + kMinShare - 1) / kMinShare;
-    ly.columns = (int)(useful < (long long)all ? useful : (long long)all);
+    const size_t all = (size_t)cut_columns(a.N, a.N_kv, false);
+    const long long useful = longest * a.B, most = cut_columns(a.N, a.N_kv, wide);
+    ly.columns = (int)(useful < most ? useful : most);
+    ly.joined = a.B < ly.columns ? a.B : ly.columns;
     char* w = static_cast<char*>(workspace);
     ly.partial = reinterpret_cast<float*>(w);
     w += all * 2 * a.N * a.D * 4;
@@ -515,8 +620,8 @@ int launch_paged_attention(hipStream_t st, const PagedAttention& a, const PagedP
     ly.joins = reinterpret_cast<int2*>(w);
   }
   const bool kv8 = a.kv_dtype == PAFU_FP8_E4M3;
-  if (a.D == 128) return kv8 ? launch<128, true>(st, a, pool, ly) : launch<128, false>(st, a, pool, ly);
-  return kv8 ? launch<64, true>(st, a, pool, ly) : launch<64, false>(st, a, pool, ly);
+  if (a.D == 128) return kv8 ? launch<128, true>(st, a, pool, ly, wide) : launch<128, false>(st, a, pool, ly, wide);
+  return kv8 ? launch<64, true>(st, a, pool, ly, wide) : launch<64, false>(st, a, pool, ly, wide);
 }
 
 }  // namespace pafu
