@@ -17,140 +17,224 @@ __device__ __forceinline__ int sat_add(int a, int b) {
   return s > 0x7fffffffu ? 0x7fffffff : (int)s;
 }
 
+// inclusive saturating sums over the wave's lanes
+__device__ __forceinline__ int wave_scan(int x) {
+  x = sat_add(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));  // row_shr:1, 2, 4, 8: within 16 lanes
+  x = sat_add(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+  x = sat_add(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+  x = sat_add(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+  x = sat_add(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));  // row_bcast:15 into rows 1 and 3
+  x = sat_add(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));  // row_bcast:31 into rows 2 and 3
+  return x;
+}
+
+__device__ __forceinline__ void load4(const int* p, int at, int n, int (&x)[4]) {  // p 16-byte aligned, at a multiple of 4
+  if (at + 4 <= n) {
+    const int4 v = *reinterpret_cast<const int4*>(p + at);
+    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = at + e < n ? p[at + e] : 0;
+  }
+}
+__device__ __forceinline__ void store4(int* p, int at, int n, const int (&x)[4]) {
+  if (at + 4 <= n) {
+    *reinterpret_cast<int4*>(p + at) = make_int4(x[0], x[1], x[2], x[3]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (at + e < n) p[at + e] = x[e];
+  }
+}
+
 // Slots (and, with TAKE, pages) for `count` tokens of each request from its token `start` on.
-//   rows: exclusive prefix sums of count -> row_start          pages: of want - have, from *free_start on -> first
-// Every workgroup forms both sums of all requests by itself (B values from L2; there is no second launch and nothing to
-// wait for) and then takes its part of the slots, four neighbouring ones per thread, whose requests it finds by bisection
-// in LDS.  A request's first new page is entered by the thread that summed it, further ones by the waves in turn.
+//   rows: exclusive sums of count -> row_start          first: of the pages wanted and not there yet, from *free_start on
+// Latency: a list of a few hundred lengths, a table entry and a slot each.  So it is one launch: every workgroup forms both
+// sums of all requests by itself, four neighbouring requests per thread (one round for 1024 requests), and keeps them in
+// LDS; then it takes its part of the table and of the slots, four neighbouring slots per thread, which finds its request by
+// bisection between those of its wave's first and last slot.  A request's first new page (a decode step has no other) is
+// entered by the thread that summed it.
 template <bool TAKE>
 __global__ __launch_bounds__(kTableThreads) void paged_tables_kernel(PagedTables t) {
   extern __shared__ int lds[];
-  int* rows = lds;             // [B + 1]
-  int* first = lds + t.B + 1;  // [B + 1] (TAKE)
+  const int stride4 = (t.B + 4) / 4 * 4;  // room for B + 1, 16-byte aligned
+  int* rows = lds;
+  int* first = lds + stride4;  // (TAKE)
   __shared__ int wave_rows[2][kTableWaves], wave_pages[2][kTableWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int page_mask = (1 << t.page_log2) - 1;
-  int row_at = 0, page_at = TAKE && t.free_start ? *t.free_start : 0;
-  if (page_at < 0) page_at = 0;
-  for (int base = 0, side = 0; base < t.B; base += kTableThreads, side ^= 1) {
-    const int b = base + tid;
-    int n = 0, have = 0, total = 0, need = 0;
-    if (b < t.B) {
-      n = max(t.count[b], 0);
-      const int s = max(t.start[b], 0);
-      total = sat_add(s, n);
-      have = (s >> t.page_log2) + ((s & page_mask) != 0);
-      need = max((total >> t.page_log2) + ((total & page_mask) != 0) - have, 0);
-    }
-    int in_rows = n, in_pages = need;  // inclusive sums
+  auto pages_of = [&](int tokens) { return (tokens >> t.page_log2) + ((tokens & page_mask) != 0); };
+  int row_at = 0, page_at = TAKE && t.free_start ? max(*t.free_start, 0) : 0;
+  for (int base = 0, side = 0; base < t.B; base += kTableThreads * 4, side ^= 1) {
+    const int b0 = base + tid * 4;
+    int n[4], s[4], total[4], need[4], sum_rows = 0, sum_pages = 0;
+    load4(t.count, b0, t.B, n);
+    if (TAKE) load4(t.start, b0, t.B, s);
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int r = __shfl_up(in_rows, d), p = __shfl_up(in_pages, d);
-      if (lane >= d) {
-        in_rows = sat_add(in_rows, r);
-        in_pages = sat_add(in_pages, p);
+    for (int e = 0; e < 4; ++e) {
+      n[e] = max(n[e], 0);
+      if (TAKE) {
+        s[e] = max(s[e], 0);
+        total[e] = sat_add(s[e], n[e]);
+        need[e] = pages_of(total[e]) - pages_of(s[e]);
+        sum_pages = sat_add(sum_pages, need[e]);
       }
+      sum_rows = sat_add(sum_rows, n[e]);
     }
+    const int in_rows = wave_scan(sum_rows), in_pages = TAKE ? wave_scan(sum_pages) : 0;
     if (lane == 63) {
       wave_rows[side][wave] = in_rows;
       wave_pages[side][wave] = in_pages;
     }
     __syncthreads();
-    int before_rows = row_at, before_pages = page_at;
+    int at_row = row_at, at_page = page_at;
 #pragma unroll
     for (int w = 0; w < kTableWaves; ++w) {
       if (w == wave) {
-        before_rows = row_at;
-        before_pages = page_at;
+        at_row = row_at;
+        at_page = page_at;
       }
       row_at = sat_add(row_at, wave_rows[side][w]);
       page_at = sat_add(page_at, wave_pages[side][w]);
     }
-    // the exclusive sum is the lower lane's inclusive one
-    int ex_rows = __shfl_up(in_rows, 1), ex_pages = __shfl_up(in_pages, 1);
-    ex_rows = sat_add(before_rows, lane ? ex_rows : 0);
-    ex_pages = sat_add(before_pages, lane ? ex_pages : 0);
-    if (b < t.B) {
-      rows[b] = ex_rows;
-      if (TAKE) first[b] = ex_pages;
-      if (blockIdx.x == 0) {
-        t.row_start[b] = ex_rows;
+    // the sum in front of this thread is the lower lane's inclusive one
+    const int lower_rows = __shfl_up(in_rows, 1), lower_pages = __shfl_up(in_pages, 1);
+    at_row = sat_add(at_row, lane ? lower_rows : 0);
+    at_page = sat_add(at_page, lane ? lower_pages : 0);
+    if (b0 < t.B) {
+      int r[4], p[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        r[e] = at_row;
+        at_row = sat_add(at_row, n[e]);
         if (TAKE) {
-          t.kv_len_out[b] = total;
-          if (need > 0 && have < t.max_pages)
-            t.table[b * t.ld_table + have] = ex_pages < t.n_free ? t.free_pages[ex_pages] : -1;
+          p[e] = at_page;
+          at_page = sat_add(at_page, need[e]);
         }
       }
+      store4(rows, b0, t.B, r);
+      if (TAKE) store4(first, b0, t.B, p);
     }
   }
   if (tid == 0) {
     rows[t.B] = row_at;
     if (TAKE) first[t.B] = page_at;
-    if (blockIdx.x == 0) {
-      t.row_start[t.B] = row_at;
-      if (TAKE) *t.free_end = page_at;
-    }
   }
   __syncthreads();
 
-  if (TAKE) {
-    // pages after a request's first new one: request by request, a request's columns over `parts` waves
-    const int waves = gridDim.x * kTableWaves, id = blockIdx.x * kTableWaves + wave;
-    const int parts = max(waves / t.B, 1);
-    for (int job = id; job < t.B * parts; job += waves) {
-      const int b = job % t.B, part = job / t.B;
-      const int need = first[b + 1] - first[b];
-      if (need <= 1 + part * 64) continue;
-      const int s = max(t.start[b], 0);
-      const int have = (s >> t.page_log2) + ((s & page_mask) != 0);
-      const int in_table = min(need, t.max_pages - have);
-      for (int i = 1 + part * 64 + lane; i < in_table; i += parts * 64) {
-        const int at = sat_add(first[b], i);
-        t.table[b * t.ld_table + have + i] = at < t.n_free ? t.free_pages[at] : -1;
-      }
-    }
-  }
-
-  const long long stride = (long long)gridDim.x * kTableThreads * 4;
-  for (long long i0 = ((long long)blockIdx.x * kTableThreads + tid) * 4; i0 < t.max_slots; i0 += stride) {
-    int b = 0, hi = t.B;  // the last request whose first row is at or before i0
-    while (hi - b > 1) {
-      const int mid = (b + hi) >> 1;
-      if (rows[mid] <= i0) b = mid;
+  // the last request whose first row is at or before row i, among lo .. hi - 1
+  auto request_of = [&](long long i, int lo, int hi) {
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (rows[mid] <= i) lo = mid;
       else hi = mid;
     }
-    int slot[4], page = -1, page_b = -1, s = 0, have = 0;
-    unsigned page_col = 0;
+    return lo;
+  };
+  const long long stride = (long long)gridDim.x * kTableThreads * 4;
+  for (long long w0 = ((long long)blockIdx.x * kTableThreads + wave * 64) * 4; w0 < t.max_slots; w0 += stride) {
+    // 64 requests at a time: where the wave's rows begin and end
+    int lo = 0, hi = t.B;
+    for (int range = hi - lo; range > 64; range = hi - lo) {
+      const int step = (range + 63) / 64, at = lo + lane * step;
+      const unsigned long long below = __ballot(at < hi && rows[min(at, t.B)] <= w0);  // lane 0 always
+      lo += (63 - __clzll(below)) * step;
+      hi = min(lo + step, hi);
+    }
+    lo = request_of(w0, lo, hi);
+    const long long i0 = w0 + lane * 4;
+    hi = lo + 1;  // past the last request that may hold a row of the wave, by steps of 64
+    while (hi < t.B) {
+      const unsigned long long in = __ballot(hi + lane < t.B && rows[min(hi + lane, t.B)] < w0 + 256);
+      hi += __popcll(in);
+      if (in != ~0ull) break;
+    }
+    int b = request_of(i0, lo, hi);
+    // four slots at once: the loads of one do not wait for another's
+    int of[4], slot[4], page[4];
+    const int* from[4];
+    unsigned token[4];
+    bool found[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int i = (int)min(i0 + e, (long long)t.max_slots - 1);
-      slot[e] = -1;
-      if (i >= row_at) continue;
-      while (i >= rows[b + 1]) ++b;
-      if (b != page_b) {
-        s = max(t.start[b], 0);
-        have = TAKE ? (s >> t.page_log2) + ((s & page_mask) != 0) : 0x7fffffff;
-      }
-      const unsigned token = (unsigned)s + (unsigned)(i - rows[b]), col = token >> t.page_log2;
-      if (b != page_b || col != page_col) {
-        page = -1;
-        if (col < (unsigned)t.max_pages) {
-          if ((int)col < have) {
-            page = t.table[b * t.ld_table + col];
-          } else {
-            const int nth = (int)col - have, at = sat_add(first[b], nth);
-            if (nth < first[b + 1] - first[b] && at < t.n_free) page = t.free_pages[at];
-          }
-        }
-        page_b = b;
-        page_col = col;
-      }
-      if (page >= 0 && page <= (0x7fffffff >> t.page_log2)) slot[e] = (page << t.page_log2) + (int)(token & page_mask);
+      found[e] = i0 + e < row_at;
+      if (found[e])
+        while (i0 + e >= rows[b + 1]) ++b;
+      of[e] = b;
     }
-    if (i0 + 4 <= t.max_slots) {
-      *reinterpret_cast<int4*>(t.slots + i0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
-    } else {
-      for (int e = 0; i0 + e < t.max_slots; ++e) t.slots[i0 + e] = slot[e];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) slot[e] = t.start[of[e]];  // (its token 0)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int s = max(slot[e], 0);
+      token[e] = (unsigned)s + (unsigned)(found[e] ? (int)(i0 + e) - rows[of[e]] : 0);
+      const unsigned col = token[e] >> t.page_log2;
+      found[e] = found[e] && col < (unsigned)t.max_pages;
+      from[e] = t.table + of[e] * t.ld_table + col;
+      if (TAKE) {
+        const int nth = (int)col - pages_of(s), at = sat_add(first[of[e]], max(nth, 0));
+        if (nth >= 0) {
+          found[e] = found[e] && nth < first[of[e] + 1] - first[of[e]] && at < t.n_free;
+          from[e] = t.free_pages + at;
+        }
+      }
+      if (!found[e]) from[e] = t.start;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) page[e] = *from[e];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      slot[e] = found[e] && page[e] >= 0 && page[e] <= (0x7fffffff >> t.page_log2)
+                    ? (page[e] << t.page_log2) + (int)(token[e] & page_mask) : -1;
+    if (i0 < t.max_slots) store4(t.slots, (int)i0, t.max_slots, slot);
+  }
+
+  // what is told by request, from the launch's last threads: a decode step's slots are the work of its first
+  const int threads = gridDim.x * kTableThreads, back = threads - 1 - (int)(blockIdx.x * kTableThreads + tid);
+  for (int b0 = back * 4; b0 < t.B; b0 += threads * 4) {
+    int r[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = rows[min(b0 + e, t.B)];
+    store4(t.row_start, b0, t.B, r);
+    if (TAKE) {
+      int n[4], s[4], total[4], page[4], at[4];
+      load4(t.count, b0, t.B, n);
+      load4(t.start, b0, t.B, s);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        at[e] = first[min(b0 + e, t.B)];
+        page[e] = at[e] < t.n_free && b0 + e < t.B ? t.free_pages[at[e]] : -1;
+        s[e] = max(s[e], 0);
+        total[e] = sat_add(s[e], max(n[e], 0));
+      }
+      store4(t.kv_len_out, b0, t.B, total);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (b0 + e < t.B && first[b0 + e + 1] > at[e] && pages_of(s[e]) < t.max_pages)
+          t.table[(b0 + e) * t.ld_table + pages_of(s[e])] = page[e];
+    }
+  }
+  if (back == 0) {
+    t.row_start[t.B] = row_at;
+    if (TAKE) *t.free_end = page_at;
+  }
+
+  if (TAKE) {
+    // pages after a request's first new one: 64 columns in a row to a wave, every parts-th run of a request's; a wave looks
+    // through 64 of its (request, run) pairs at once for those that are not empty
+    const int waves = gridDim.x * kTableWaves, id = blockIdx.x * kTableWaves + wave, parts = max(waves / t.B, 1);
+    const int jobs = t.B * parts;
+    for (int j0 = id; j0 < jobs; j0 += waves * 64) {
+      const int j = j0 + lane * waves, mine = j < jobs ? j % t.B : 0;
+      for (unsigned long long todo = __ballot(j < jobs && first[mine + 1] - first[mine] > 1 + j / t.B * 64); todo;
+           todo &= todo - 1) {
+        const int job = j0 + (__ffsll(todo) - 1) * waves, b = job % t.B, part = job / t.B, begin = first[b];
+        const int have = pages_of(max(t.start[b], 0)), in_table = min(first[b + 1] - begin, t.max_pages - have);
+        for (int i = 1 + part * 64 + lane; i < in_table; i += parts * 64) {
+          const int at = sat_add(begin, i);
+          t.table[b * t.ld_table + have + i] = at < t.n_free ? t.free_pages[at] : -1;
+        }
+      }
     }
   }
 }
@@ -197,11 +281,11 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const char* __restric
 }  // namespace
 
 int launch_paged_tables(hipStream_t st, const PagedTables& t, bool take_pages) {
-  // a workgroup per 1024 slots, at most two per compute unit: each forms the sums of all requests
+  // a workgroup per 1024 slots, at most four per compute unit
   long long blocks = ((long long)t.max_slots + kTableThreads * 4 - 1) / (kTableThreads * 4);
-  const long long most = 2ll * compute_units();
+  const long long most = 4ll * compute_units();
   blocks = blocks < 1 ? 1 : (blocks > most ? most : blocks);
-  const size_t lds = (size_t)(t.B + 1) * 4 * (take_pages ? 2 : 1);
+  const size_t lds = (size_t)(t.B + 4) / 4 * 16 * (take_pages ? 2 : 1);
   if (take_pages)
     hipLaunchKernelGGL(paged_tables_kernel<true>, dim3((unsigned)blocks), dim3(kTableThreads), lds, st, t);
   else
