@@ -440,69 +440,76 @@ def pafu_sse_score(Q, K, block_len, out, workspace, softmax_scale=0.0, stream=No
 # ---- paged K/V cache.  Lengths, tables and slots are read on the device, so what the C side cannot see of them (their
 # type, size and device) is checked here.
 
-def _on_current_device(*tensors):
+def _paged_stream(stream, *tensors):
+    """The stream of a call whose tensors (None: not given) all lie on the current device."""
     import torch
     device = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("the tensors are on different devices")
     if device < 0:
         raise ValueError("the tensors must be on the GPU")
     if device != torch.cuda.current_device():
         raise ValueError("the tensors are on GPU %d and the current device is %d" % (device, torch.cuda.current_device()))
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError("the tensors are on different devices")
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
 
 
 def _int32_list(name, t, n=None):
     import torch
+    shape = t.shape
     if t.dtype is not torch.int32:
         raise TypeError("%s must be int32, not %s" % (name, t.dtype))
-    if t.dim() != 1 or (t.shape[0] > 1 and t.stride(0) != 1) or (n is not None and t.shape[0] != n):
+    if len(shape) != 1 or not t.is_contiguous() or (n is not None and shape[0] != n):
         raise ValueError("%s must be a contiguous list%s, not %s with strides %s"
-                         % (name, "" if n is None else " of %d" % n, tuple(t.shape), t.stride()))
+                         % (name, "" if n is None else " of %d" % n, tuple(shape), t.stride()))
     return t.data_ptr()
 
 
 def _block_table(t, n):
     import torch
+    shape, strides = t.shape, t.stride()
     if t.dtype is not torch.int32:
         raise TypeError("the block table must be int32, not %s" % t.dtype)
-    if t.dim() != 2 or t.shape[0] != n or (t.shape[1] > 1 and t.stride(1) != 1):
+    if len(shape) != 2 or shape[0] != n or (shape[1] > 1 and strides[1] != 1):
         raise ValueError("the block table must be [%d, max_pages] with contiguous rows, not %s with strides %s"
-                         % (n, tuple(t.shape), t.stride()))
-    columns = t.shape[1]
-    return t.data_ptr(), columns, t.stride(0) if n > 1 else max(columns, 1)
+                         % (n, tuple(shape), strides))
+    return t.data_ptr(), shape[1], strides[0] if n > 1 else max(shape[1], 1)
 
 
 def _pool_dtype(K_pages, V_pages):
     """dtype code of a page pool after the checks that need its shape: both tensors alike, elements contiguous."""
     import torch
-    shape, strides = K_pages.shape, K_pages.stride()
+    shape, strides, dtype = K_pages.shape, K_pages.stride(), K_pages.dtype
     if len(shape) != 4 or V_pages.shape != shape or V_pages.stride() != strides or strides[3] != 1:
         raise ValueError("the page tensors must be [n_pages, page_size, N_kv, D] of one shape and stride, elements contiguous")
-    if V_pages.dtype is not K_pages.dtype or K_pages.dtype not in (torch.bfloat16, torch.uint8):
-        raise TypeError("page tensors are bfloat16 or uint8 (E4M3 codes), not %s and %s" % (K_pages.dtype, V_pages.dtype))
-    return PAFU_BF16 if K_pages.dtype is torch.bfloat16 else PAFU_FP8_E4M3
+    if V_pages.dtype is dtype:
+        if dtype is torch.bfloat16:
+            return PAFU_BF16
+        if dtype is torch.uint8:
+            return PAFU_FP8_E4M3
+    raise TypeError("page tensors are bfloat16 or uint8 (E4M3 codes), not %s and %s" % (dtype, V_pages.dtype))
 
 
 def _rows_3d(name, t, dtypes):
     """[rows, heads, D] with contiguous rows of one of `dtypes` -> token stride."""
+    shape, strides = t.shape, t.stride()
     if t.dtype not in dtypes:
         raise TypeError("%s has the unsupported dtype %s" % (name, t.dtype))
-    if t.dim() != 3:
-        raise ValueError("%s must be [rows, heads, D], not %s" % (name, tuple(t.shape)))
-    rows, heads, D = t.shape
-    if (D > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != D):
-        raise ValueError("%s must have contiguous rows, not strides %s" % (name, t.stride()))
-    return t.stride(0) if rows > 1 else heads * D
+    if len(shape) != 3:
+        raise ValueError("%s must be [rows, heads, D], not %s" % (name, tuple(shape)))
+    rows, heads, D = shape
+    if (D > 1 and strides[2] != 1) or (heads > 1 and strides[1] != D):
+        raise ValueError("%s must have contiguous rows, not strides %s" % (name, strides))
+    return strides[0] if rows > 1 else heads * D
 
 
 def pafu_paged_tables(kv_len, new_len, free_pages, page_size, block_table, slots, row_start, kv_len_out, free_end,
                       free_start=None, stream=None):
     """Pages from free_pages for every request's new tokens, entered in block_table [B, max_pages], and their slots."""
     B = kv_len.shape[0]
-    _on_current_device(kv_len, new_len, free_pages, block_table, slots, row_start, kv_len_out, free_end, free_start)
+    st = _paged_stream(stream, kv_len, new_len, free_pages, block_table, slots, row_start, kv_len_out, free_end, free_start)
     table, max_pages, ld_table = _block_table(block_table, B)
-    rc = _lib().pafu_paged_tables(_stream(stream), _int32_list("kv_len", kv_len), _int32_list("new_len", new_len, B), B,
+    rc = _lib().pafu_paged_tables(st, _int32_list("kv_len", kv_len), _int32_list("new_len", new_len, B), B,
                                   _int32_list("free_pages", free_pages), free_pages.shape[0],
                                   None if free_start is None else _int32_list("free_start", free_start, 1), page_size,
                                   table, max_pages, ld_table, _int32_list("slots", slots), slots.shape[0],
@@ -515,9 +522,9 @@ def pafu_paged_tables(kv_len, new_len, free_pages, page_size, block_table, slots
 def pafu_paged_slots(block_table, start, count, page_size, slots, row_start, stream=None):
     """Slots of the tokens start[b] .. start[b] + count[b] - 1 of every request, request after request."""
     B = start.shape[0]
-    _on_current_device(block_table, start, count, slots, row_start)
+    st = _paged_stream(stream, block_table, start, count, slots, row_start)
     table, max_pages, ld_table = _block_table(block_table, B)
-    rc = _lib().pafu_paged_slots(_stream(stream), table, max_pages, ld_table, _int32_list("start", start),
+    rc = _lib().pafu_paged_slots(st, table, max_pages, ld_table, _int32_list("start", start),
                                  _int32_list("count", count, B), B, page_size, _int32_list("slots", slots), slots.shape[0],
                                  _int32_list("row_start", row_start, B + 1))
     _check(rc, "pafu_paged_slots")
@@ -528,7 +535,7 @@ def pafu_paged_append(K, V, slots, K_pages, V_pages, k_scale_log2=0, v_scale_log
     """K, V: [rows, N, D] bf16 -> K_pages, V_pages: [n_pages, page_size, N, D] bf16, or uint8 E4M3 codes of value /
     2^scale_log2, at the rows' slots (int32; a slot outside the pool leaves its row out)."""
     import torch
-    _on_current_device(K, V, slots, K_pages, V_pages)
+    st = _paged_stream(stream, K, V, slots, K_pages, V_pages)
     kv_dtype = _pool_dtype(K_pages, V_pages)
     n_pages, page_size, N, D = K_pages.shape
     ld_in = _rows_3d("K", K, (torch.bfloat16,))
@@ -536,7 +543,7 @@ def pafu_paged_append(K, V, slots, K_pages, V_pages, k_scale_log2=0, v_scale_log
     if K.shape[1] != N or K.shape[2] != D or V.shape != K.shape or _rows_3d("V", V, (torch.bfloat16,)) != ld_in:
         raise ValueError("K and V must be [rows, %d, %d] with one stride, not %s and %s" % (N, D, tuple(K.shape), tuple(V.shape)))
     ld = K_pages.stride()
-    rc = _lib().pafu_paged_append(_stream(stream), K.data_ptr(), V.data_ptr(), ld_in, rows, _int32_list("slots", slots, rows),
+    rc = _lib().pafu_paged_append(st, K.data_ptr(), V.data_ptr(), ld_in, rows, _int32_list("slots", slots, rows),
                                   N, D, K_pages.data_ptr(), V_pages.data_ptr(), n_pages, page_size, ld[0], ld[1], ld[2],
                                   kv_dtype, k_scale_log2, v_scale_log2)
     _check(rc, "pafu_paged_append")
@@ -551,19 +558,25 @@ def pafu_paged_attention(Q, K_pages, V_pages, block_table, kv_len, O, n_pinned=0
                          k_scale_log2=0, v_scale_log2=0, workspace=None, stream=None):
     """Q, O: [B, N, D], one new token per request; K_pages, V_pages: [n_pages, page_size, N_kv, D] bf16 or uint8 codes."""
     import torch
-    _on_current_device(Q, K_pages, V_pages, block_table, kv_len, O, workspace)
+    st = _paged_stream(stream, Q, K_pages, V_pages, block_table, kv_len, O, workspace)
     kv_dtype = _pool_dtype(K_pages, V_pages)
     n_pages, page_size, N_kv, D = K_pages.shape
     ld_q, ld_o = _rows_3d("Q", Q, (torch.bfloat16,)), _rows_3d("O", O, (torch.bfloat16, torch.float32))
-    B, N = Q.shape[0], Q.shape[1]
-    if Q.shape[2] != D or O.shape != Q.shape:
+    shape = Q.shape
+    B, N = shape[0], shape[1]
+    if shape[2] != D or O.shape != shape:
         raise ValueError("Q and O must be [B, N, %d], not %s and %s" % (D, tuple(Q.shape), tuple(O.shape)))
     table, max_pages, ld_table = _block_table(block_table, B)
     ld = K_pages.stride()
-    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    rc = _lib().pafu_paged_attention(_stream(stream), Q.data_ptr(), ld_q, K_pages.data_ptr(), V_pages.data_ptr(), n_pages,
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("the workspace must be contiguous")
+        ws, ws_bytes = workspace.data_ptr(), workspace.nbytes
+    rc = _lib().pafu_paged_attention(st, Q.data_ptr(), ld_q, K_pages.data_ptr(), V_pages.data_ptr(), n_pages,
                                      page_size, ld[0], ld[1], ld[2], kv_dtype, k_scale_log2, v_scale_log2, table, max_pages,
                                      ld_table, _int32_list("kv_len", kv_len, B), B, N, N_kv, D, n_pinned, window,
-                                     float(softmax_scale), O.data_ptr(), ld_o, _dtype_code(O), _ptr(workspace), ws_bytes)
+                                     float(softmax_scale), O.data_ptr(), ld_o,
+                                     PAFU_BF16 if O.dtype is torch.bfloat16 else PAFU_F32, ws, ws_bytes)
     _check(rc, "pafu_paged_attention")
     return O
