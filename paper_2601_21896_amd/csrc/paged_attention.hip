@@ -82,12 +82,21 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
-// A tile's raw rows as one lane holds them.
+// A tile's rows as one lane reads them.
 template <int D, bool KV8>
 struct Raw {
-  static constexpr int kK = KV8 ? D / 64 : D / 32;        // 16-byte pieces of a K row
-  static constexpr int kVWords = KV8 ? D / 64 : D / 32;   // 32-bit words of a V row: D / 16 elements
-  u32x4 k[2][kK];
+  static constexpr int kRow = KV8 ? D : 2 * D;            // bytes
+  static constexpr int kK = kRow / 64;                    // 16-byte pieces of a lane's part of a K row
+  static constexpr int kVWords = kRow / 64;               // 32-bit words of its part of a V row: D / 16 elements
+  // K is read 16 bytes a lane, kLanes lanes to a row (each of the four lane groups kStep rows at once), and turned in LDS, a
+  // row 16 bytes longer there to spread the banks.  Read the way the matrix instruction wants it (16 rows and 64 bytes of
+  // each at a time) the 8-bit cache of 12 x 128 came at 6.1 TB/s instead of 6.7, the bf16 one of 8 x 128 at 6.80 instead
+  // of 6.85; pages of 16 tokens 5 % slower, since K and V no longer share a lane's page.
+  static constexpr int kLanes = kRow / 16, kStep = 16 / kLanes, kPitch = kRow + 16;
+  // Lane group g's part of a row: 32 neighbouring bytes of every 128 (of a row of 64 bytes 16).
+  static constexpr int kPiece = kRow == 64 ? 16 : 32;
+  static __device__ constexpr int at(int i) { return (i >> 1) * 128 + (i & 1) * 16; }
+  u32x4 k[2 * kK];
   unsigned v[8][kVWords];
 };
 
@@ -111,6 +120,13 @@ __device__ __forceinline__ void load_words(const char* p, unsigned (&w)[WORDS]) 
   }
 }
 
+// LDS that a wave alone uses: its accesses are carried out in order, so only the compiler has to keep to it.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // two codes of a word -> two bf16 (exact; the tensor's scale is applied elsewhere)
 __device__ __forceinline__ unsigned widen2(unsigned w, bool upper) {
   return upper ? __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true))
@@ -124,18 +140,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
   constexpr bool kOnce = QT == 1;  // K and V are read by one wave only
   using R = Raw<D, KV8>;
   constexpr int kWays = WIDE ? kWaves : 1;
-  __shared__ f32x4 part[kWays][QT][4][kBlocks / 4][WIDE ? 64 : 1];
+  // K on its way to the matrix instructions, then what the waves of a wide workgroup add up
+  constexpr int kStage = kWaves * kTile * R::kPitch, kParts = WIDE ? kWaves * QT * kBlocks * 64 * 16 : 0;
+  __shared__ __attribute__((aligned(16))) char lds[kStage > kParts ? kStage : kParts];
+  f32x4 (*part)[QT][4][kBlocks / 4][64] = reinterpret_cast<f32x4 (*)[QT][4][kBlocks / 4][64]>(lds);
   __shared__ float2 part_stat[kWays][QT][16];
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = a.N / a.N_kv, out_bytes = a.out_dtype == PAFU_F32 ? 4 : 2;
 
   // ---- the tiles of all requests
-  int total = 0, mine = 0, ends = 0;  // mine, ends: of request `lane`, the last ones summed
+  int total = 0, kv = 0, mine = 0, ends = 0;  // of request `lane`: its length, its tiles, theirs and those before it
   if (ly.cut) {
     for (int r0 = 0; r0 < a.B; r0 += 64) {
-      const int r = r0 + lane;
-      mine = r < a.B ? request_tiles(a, pool.page_log2, a.kv_len[r]).n : 0;
+      kv = a.kv_len[min(r0 + lane, a.B - 1)];
+      mine = r0 + lane < a.B ? request_tiles(a, pool.page_log2, kv).n : 0;
       ends = total + wave_scan(mine);
       total = __builtin_amdgcn_readlane(ends, 63);
     }
@@ -157,8 +176,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
       left = min(share, total - (int)first);
       for (int r0 = 0;; r0 += 64) {
         if (a.B > 64) {
-          const int r = r0 + lane;
-          mine = r < a.B ? request_tiles(a, pool.page_log2, a.kv_len[r]).n : 0;
+          kv = a.kv_len[min(r0 + lane, a.B - 1)];
+          mine = r0 + lane < a.B ? request_tiles(a, pool.page_log2, kv).n : 0;
           ends = before + wave_scan(mine);
         }
         const unsigned long long beyond = __ballot(ends > (int)first);
@@ -166,6 +185,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
           const int l = __ffsll(beyond) - 1;
           b = r0 + l;
           before = __builtin_amdgcn_readlane(ends - mine, l);
+          kv = __builtin_amdgcn_readlane(kv, l);
           at = (int)first - before;
           break;
         }
@@ -176,25 +196,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
 
   // joins are told by request, or by column with the request in the first place
   const bool by_request = ly.cut && ly.joined == a.B, tells = ly.cut && head_id == 0 && sub == 0 && lane == 0;
-  // ---- requests without tiles
-  for (int r = x; r < a.B; r += columns) {
-    if (request_tiles(a, pool.page_log2, a.kv_len[r]).n > 0) continue;
-    const int h0 = kvh * G + group * 16 * QT, rows = min(16 * QT, G - group * 16 * QT);
-    char* to = static_cast<char*>(a.O) + r * a.ld_o + (long long)h0 * D * out_bytes;
-    if (sub == 0)
-      for (int i = lane; i < rows * D * out_bytes / 16; i += 64) reinterpret_cast<u32x4*>(to)[i] = u32x4{0, 0, 0, 0};
-    if (by_request && tells) ly.joins[r] = make_int2(0, 0);
-  }
-
   const float sc = a.scale * a.k_scale * kLog2e;
   int2 join = make_int2(0, 0);  // of the column
-  while (left > 0 && b < a.B) {
-    const Tiles t = request_tiles(a, pool.page_log2, a.kv_len[b]);
+  if (!ly.cut) kv = a.kv_len[b];
+  while (left > 0) {
+    const Tiles t = request_tiles(a, pool.page_log2, __builtin_amdgcn_readfirstlane(kv));
     const int here = min(t.n - at, left);
     if (here <= 0) {  // no tiles
-      if (!ly.cut) break;
-      before += t.n;
-      ++b;
+      if (!ly.cut || ++b == a.B) break;
+      kv = a.kv_len[b];
       at = 0;
       continue;
     }
@@ -207,7 +217,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
       const char* qp = static_cast<const char*>(a.Q) + b * a.ld_q + ((long long)kvh * G + hq) * (D * 2);
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
-        const int d = KV8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8;
+        const int d = KV8 ? g * (D / 4) + s * 8 : (s >> 1) * 64 + g * 16 + (s & 1) * 8;
         q[qt][s] = *reinterpret_cast<const bf16x8*>(qp + d * 2);
       }
     }
@@ -221,66 +231,66 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
       for (int i = 0; i < kBlocks; ++i) o[qt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // ---- addresses: a group of eight tokens lies on one page
+    // ---- addresses: lane group g reads tokens 8 g .. 8 g + 7 of a tile, which lie on one page
     const int* row = a.table + b * a.ld_table;
-    const int kgroup = n >> 2;  // the group that this lane's K rows belong to
     const long long head = kvh * pool.ld_head;
-    const char* Kl = pool.K + head + (n & 3) * pool.ld_token + g * 16;
-    const char* Vl = pool.V + head + n * (D / 16) * (KV8 ? 1 : 2);
+    const char* Kl = pool.K + head + (n / R::kLanes) * pool.ld_token + (n % R::kLanes) * 16;
+    const char* Vl = pool.V + head + n * (R::kRow / 16);
+    char* k_in = lds + wave * (kTile * R::kPitch) + (g * 8 + n / R::kLanes) * R::kPitch + (n % R::kLanes) * 16;
+    const char* k_out = lds + wave * (kTile * R::kPitch) + ((n >> 2) * 8 + (n & 3)) * R::kPitch + g * R::kPiece;
     const int mask = (1 << pool.page_log2) - 1;
     auto tile_base = [&](int i) { return i < t.n_pin ? i * kTile : t.base + (i - t.n_pin) * kTile; };
-    auto page_at = [&](int token) { return row[min(token >> pool.page_log2, a.max_pages - 1)]; };
-    auto offset = [&](int page, int token) {
-      page = max(min(page, pool.n_pages - 1), 0);
-      return page * pool.ld_page + (token & mask) * pool.ld_token;
-    };
-    // Where a wave's next tile lies; behind its last one the first row of the pool, one line for all lanes: loads on every path,
-    // in one order, let the compiler wait for just the ones it needs.
-    auto k_at = [&](int base, int page, bool there) { return there ? Kl + offset(page, base + kgroup * 8) : pool.K; };
-    auto v_at = [&](int base, int page, bool there) { return there ? Vl + offset(page, base + g * 8) : pool.V; };
-    auto load_k = [&](R& raw, const char* p) {
-#pragma unroll
-      for (int tk = 0; tk < 2; ++tk)
-#pragma unroll
-        for (int i = 0; i < R::kK; ++i) raw.k[tk][i] = load<kOnce, u32x4>(p + tk * 4 * pool.ld_token + i * 64);
-    };
-    auto load_v = [&](R& raw, const char* p) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) load_words<kOnce>(p + j * pool.ld_token, raw.v[j]);
-    };
     auto nth = [&](int i) { return tile_base(at + min(i, here - 1)); };
-
-    // Pages are asked for two tiles ahead, K and V one, always in the order K, pages, V: the wait for K then leaves V in flight.
+    auto page_of = [&](int base) { return row[min((base + g * 8) >> pool.page_log2, a.max_pages - 1)]; };
     auto in_pool = [&](int page) { return page >= 0 && page < pool.n_pages; };
+    // Where this lane's rows lie; behind the last tile the first row of the pool, one line for all lanes: loads on every path, in
+    // one order, let the compiler wait for just the ones it needs.
+    auto offset = [&](int base, int page) {
+      page = max(min(page, pool.n_pages - 1), 0);
+      return page * pool.ld_page + ((base + g * 8) & mask) * pool.ld_token;
+    };
+    auto load_k = [&](R& raw, const char* from) {
+#pragma unroll
+      for (int i = 0; i < 2 * R::kK; ++i) raw.k[i] = load<kOnce, u32x4>(from + i * R::kStep * pool.ld_token);
+    };
+    auto load_v = [&](R& raw, const char* from) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) load_words<kOnce>(from + j * pool.ld_token, raw.v[j]);
+    };
+
+    // A tile's page is asked for two tiles ahead, its rows one, always in the order K, page, V: the wait for K then leaves V in
+    // flight.  (Rows two tiles ahead gained nothing anywhere.)
     R raw;
     int base = nth(sub), base1 = nth(sub + kWays);
-    int page_v = page_at(base + g * 8), page_k = page_at(base + kgroup * 8);
-    bool page_ok = in_pool(page_v);
-    const char *k_next = k_at(base, page_k, sub < here), *v_next = v_at(base, page_v, sub < here);
-    page_v = page_at(base1 + g * 8);
-    page_k = page_at(base1 + kgroup * 8);
+    int page = page_of(base);
+    bool page_ok = in_pool(page);
+    long long from = offset(base, page);
+    page = page_of(base1);
     __builtin_amdgcn_sched_barrier(0);
-    load_k(raw, k_next);
+    load_k(raw, sub < here ? Kl + from : pool.K);
     __builtin_amdgcn_sched_barrier(0);
-    load_v(raw, v_next);
+    load_v(raw, sub < here ? Vl + from : pool.V);
     __builtin_amdgcn_sched_barrier(0);
 
     for (int i = sub; i < here; i += kWays) {
       const bool more = i + kWays < here;
       // ---- S^T = K Q^T
+      wave_sync();
+#pragma unroll
+      for (int j = 0; j < 2 * R::kK; ++j) *reinterpret_cast<u32x4*>(k_in + j * R::kStep * R::kPitch) = raw.k[j];
+      wave_sync();
       f32x4 s[QT][2];
 #pragma unroll
       for (int tk = 0; tk < 2; ++tk) {
         bf16x8 k[kSteps];
 #pragma unroll
-        for (int e = 0; e < kSteps; ++e) {
+        for (int j = 0; j < R::kK; ++j) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(k_out + tk * 4 * R::kPitch + R::at(j));
           if constexpr (KV8) {
-            u32x4 w;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) w[u] = widen2(raw.k[tk][e >> 1][(e & 1) * 2 + (u >> 1)], u & 1);
-            k[e] = __builtin_bit_cast(bf16x8, w);
+            k[2 * j] = __builtin_bit_cast(bf16x8, u32x4{widen2(x[0], false), widen2(x[0], true), widen2(x[1], false), widen2(x[1], true)});
+            k[2 * j + 1] = __builtin_bit_cast(bf16x8, u32x4{widen2(x[2], false), widen2(x[2], true), widen2(x[3], false), widen2(x[3], true)});
           } else {
-            k[e] = __builtin_bit_cast(bf16x8, raw.k[tk][e]);
+            k[j] = __builtin_bit_cast(bf16x8, x);
           }
         }
 #pragma unroll
@@ -291,13 +301,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
             s[qt][tk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[e], q[qt][e], s[qt][tk], 0, 0, 0);
         }
       }
-      k_next = k_at(base1, page_k, more);
-      v_next = v_at(base1, page_v, more);
-      const bool next_ok = in_pool(page_v);
+      const long long next = offset(base1, page);
+      const bool next_ok = in_pool(page);
       const int base2 = nth(i + 2 * kWays);
-      load_k(raw, k_next);
-      page_v = page_at(base2 + g * 8);
-      page_k = page_at(base2 + kgroup * 8);
+      load_k(raw, more ? Kl + next : pool.K);
+      page = page_of(base2);
 
       // ---- what is not visible: s(tk, r) belongs to token base + 8 g + 4 tk + r, V's row j to base + 8 g + j
       const bool pinned = at + i < t.n_pin;
@@ -367,7 +375,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
           o[qt][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, lo_w[qt], o[qt][k], 0, 0, 0);
         }
       }
-      load_v(raw, v_next);
+      load_v(raw, more ? Vl + next : pool.V);
       base = base1;
       base1 = base2;
       page_ok = next_ok;
@@ -383,7 +391,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
     const bool whole = at == 0 && here == t.n;
     const long long slot = 2ll * x + (at == 0 ? 1 : 0);
     if constexpr (WIDE) {
-      __syncthreads();  // the sums of the piece before are formed
+      __syncthreads();  // no wave has K in LDS any more
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
 #pragma unroll
@@ -463,10 +471,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
     }
     left -= here;
     before += t.n;
-    ++b;
     at = 0;
+    if (left <= 0 || ++b == a.B) break;
+    if constexpr (WIDE) __syncthreads();  // the sums are formed: K may come again
+    kv = a.kv_len[b];
   }
   if (tells && !by_request) ly.joins[x] = join;
+
+  // ---- requests without tiles
+  for (int r = x; r < a.B; r += columns) {
+    if (request_tiles(a, pool.page_log2, a.kv_len[r]).n > 0) continue;
+    const int h0 = kvh * G + group * 16 * QT, rows = min(16 * QT, G - group * 16 * QT);
+    char* to = static_cast<char*>(a.O) + r * a.ld_o + (long long)h0 * D * out_bytes;
+    if (sub == 0)
+      for (int i = lane; i < rows * D * out_bytes / 16; i += 64) reinterpret_cast<u32x4*>(to)[i] = u32x4{0, 0, 0, 0};
+    if (by_request && tells) ly.joins[r] = make_int2(0, 0);
+  }
 }
 
 // Joins the partial results of a request that is cut: one workgroup per (request, query head), D / 4 lanes to a partial
@@ -546,14 +566,17 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttention a, Layou
   }
 }
 
-int query_tiles(int G) { return G <= 16 ? 1 : 2; }
-int head_waves(int N, int N_kv) {
-  const int G = N / N_kv, rows = 16 * query_tiles(G);
-  return N_kv * ((G + rows - 1) / rows);
+// Query heads of a key head: `groups` of up to 16 * qt.
+struct Groups {
+  int qt, groups;
+};
+Groups query_groups(int N, int N_kv, int D) {
+  const int tiles = (N / N_kv + 15) / 16, most = D == 64 ? 3 : 2, groups = (tiles + most - 1) / most;
+  return {(tiles + groups - 1) / groups, groups};
 }
 // Columns of a cut launch: eight waves per compute unit, which are all there at once.
-int cut_columns(int N, int N_kv, bool wide) {
-  const int columns = 8 * compute_units() / (wide ? kWaves : 1) / head_waves(N, N_kv);
+int cut_columns(int heads, bool wide) {
+  const int columns = 8 * compute_units() / (wide ? kWaves : 1) / heads;
   return columns < 1 ? 1 : columns;
 }
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
@@ -579,22 +602,26 @@ int launch(hipStream_t st, const PagedAttention& a, const PagedPool& pool, const
 }
 template <int D, bool KV8>
 int launch(hipStream_t st, const PagedAttention& a, const PagedPool& pool, const Layout& ly, bool wide) {
-  return query_tiles(a.N / a.N_kv) == 1 ? launch<D, KV8, 1>(st, a, pool, ly, wide) : launch<D, KV8, 2>(st, a, pool, ly, wide);
+  switch (query_groups(a.N, a.N_kv, D).qt) {
+    case 1: return launch<D, KV8, 1>(st, a, pool, ly, wide);
+    case 2: return launch<D, KV8, 2>(st, a, pool, ly, wide);
+    default: return launch<64, KV8, 3>(st, a, pool, ly, wide);  // (D is 64)
+  }
 }
 
 }  // namespace
 
 size_t paged_attention_workspace_bytes(int B, int N, int N_kv, int D) {
   (void)B;
-  const size_t columns = (size_t)cut_columns(N, N_kv, false), rows = columns * 2 * N;
+  const size_t columns = (size_t)cut_columns(N_kv * query_groups(N, N_kv, D).groups, false), rows = columns * 2 * N;
   return rows * D * 4 + round16(rows * 8) + round16(columns * 8);
 }
 
 int launch_paged_attention(hipStream_t st, const PagedAttention& a, const PagedPool& pool, void* workspace,
                            size_t workspace_bytes) {
   Layout ly;
-  ly.heads = head_waves(a.N, a.N_kv);
-  ly.groups = ly.heads / a.N_kv;
+  ly.groups = query_groups(a.N, a.N_kv, a.D).groups;
+  ly.heads = a.N_kv * ly.groups;
   const long long longest = ((((long long)a.max_pages << pool.page_log2) + kTile - 1) / kTile);
   ly.cut = workspace != nullptr && workspace_bytes >= paged_attention_workspace_bytes(a.B, a.N, a.N_kv, a.D) &&
            longest > kMinShare;
@@ -608,8 +635,8 @@ int launch_paged_attention(hipStream_t st, const PagedAttention& a, const PagedP
   const bool wide = ly.cut ? ly.heads < kWaves || pool.ld_head > pool.ld_token
                            : longest >= kLong || (long long)a.B * ly.heads <= 2ll * compute_units();
   if (ly.cut) {
-    const size_t all = (size_t)cut_columns(a.N, a.N_kv, false);
-    const long long useful = longest * a.B, most = cut_columns(a.N, a.N_kv, wide);
+    const size_t all = (size_t)cut_columns(ly.heads, false);
+    const long long useful = longest * a.B, most = cut_columns(ly.heads, wide);
     ly.columns = (int)(useful < most ? useful : most);
     ly.joined = a.B < ly.columns ? a.B : ly.columns;
     char* w = static_cast<char*>(workspace);
