@@ -240,11 +240,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
     const char* k_out = lds + wave * (kTile * R::kPitch) + ((n >> 2) * 8 + (n & 3)) * R::kPitch + g * R::kPiece;
     const int mask = (1 << pool.page_log2) - 1;
     auto tile_base = [&](int i) { return i < t.n_pin ? i * kTile : t.base + (i - t.n_pin) * kTile; };
-    auto nth = [&](int i) { return tile_base(at + min(i, here - 1)); };
+    auto nth = [&](int i) { return min(at + i, at + here - 1); };
     auto page_of = [&](int base) { return row[min((base + g * 8) >> pool.page_log2, a.max_pages - 1)]; };
-    auto in_pool = [&](int page) { return page >= 0 && page < pool.n_pages; };
-    // Where this lane's rows lie; behind the last tile the first row of the pool, one line for all lanes: loads on every path, in
-    // one order, let the compiler wait for just the ones it needs.
+    // is any of this lane's eight tokens of tile i visible, on a page of the pool?
+    auto seen = [&](int i, int base, int page) {
+      const int first = base + g * 8;
+      return page >= 0 && page < pool.n_pages && first + 7 >= (i < t.n_pin ? 0 : t.lo) && first < (i < t.n_pin ? t.pin : t.len);
+    };
+    // Where this lane's rows lie.  Rows that are not seen, and those behind the last tile, are the pool's first: one line for
+    // all, and loads on every path, in one order, let the compiler wait for just the ones it needs.
     auto offset = [&](int base, int page) {
       page = max(min(page, pool.n_pages - 1), 0);
       return page * pool.ld_page + ((base + g * 8) & mask) * pool.ld_token;
@@ -261,15 +265,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
     // A tile's page is asked for two tiles ahead, its rows one, always in the order K, page, V: the wait for K then leaves V in
     // flight.  (Rows two tiles ahead gained nothing anywhere.)
     R raw;
-    int base = nth(sub), base1 = nth(sub + kWays);
+    int tile = nth(sub), base = tile_base(tile), tile1 = nth(sub + kWays), base1 = tile_base(tile1);
     int page = page_of(base);
-    bool page_ok = in_pool(page);
-    long long from = offset(base, page);
+    bool ok = seen(tile, base, page);
+    const long long from = offset(base, page);
     page = page_of(base1);
     __builtin_amdgcn_sched_barrier(0);
-    load_k(raw, sub < here ? Kl + from : pool.K);
+    load_k(raw, ok && sub < here ? Kl + from : pool.K);
     __builtin_amdgcn_sched_barrier(0);
-    load_v(raw, sub < here ? Vl + from : pool.V);
+    load_v(raw, ok && sub < here ? Vl + from : pool.V);
     __builtin_amdgcn_sched_barrier(0);
 
     for (int i = sub; i < here; i += kWays) {
@@ -302,23 +306,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
         }
       }
       const long long next = offset(base1, page);
-      const bool next_ok = in_pool(page);
-      const int base2 = nth(i + 2 * kWays);
-      load_k(raw, more ? Kl + next : pool.K);
+      const bool next_ok = seen(tile1, base1, page), there = next_ok && more;
+      const int tile2 = nth(i + 2 * kWays), base2 = tile_base(tile2);
+      load_k(raw, there ? Kl + next : pool.K);
       page = page_of(base2);
 
       // ---- what is not visible: s(tk, r) belongs to token base + 8 g + 4 tk + r, V's row j to base + 8 g + j
-      const bool pinned = at + i < t.n_pin;
+      const bool pinned = tile < t.n_pin;
       const int lo = pinned ? 0 : t.lo, hi = pinned ? t.pin : t.len;
-      if (base < lo || hi - base < kTile || __ballot(!page_ok)) {
+      if (base < lo || hi - base < kTile || __ballot(!ok)) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int token = base + g * 8 + j;
-          const bool seen = page_ok && token >= lo && token < hi;
+          const bool visible = ok && token >= lo && token < hi;
 #pragma unroll
-          for (int qt = 0; qt < QT; ++qt) s[qt][j >> 2][j & 3] = seen ? s[qt][j >> 2][j & 3] : -__builtin_inff();
+          for (int qt = 0; qt < QT; ++qt) s[qt][j >> 2][j & 3] = visible ? s[qt][j >> 2][j & 3] : -__builtin_inff();
 #pragma unroll
-          for (int w = 0; w < R::kVWords; ++w) raw.v[j][w] = seen ? raw.v[j][w] : 0u;
+          for (int w = 0; w < R::kVWords; ++w) raw.v[j][w] = visible ? raw.v[j][w] : 0u;
         }
       }
 
@@ -375,10 +379,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
           o[qt][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, lo_w[qt], o[qt][k], 0, 0, 0);
         }
       }
-      load_v(raw, more ? Vl + next : pool.V);
+      load_v(raw, there ? Vl + next : pool.V);
+      tile = tile1;
       base = base1;
+      tile1 = tile2;
       base1 = base2;
-      page_ok = next_ok;
+      ok = next_ok;
     }
 
     // ---- out: lane (g, n) holds query n's elements (4 g + r) * kBlocks + k.  The waves of a wide workgroup leave what they
