@@ -149,15 +149,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = a.N / a.N_kv, out_bytes = a.out_dtype == PAFU_F32 ? 4 : 2;
 
-  // ---- the tiles of all requests
-  int total = 0, kv = 0, mine = 0, ends = 0;  // of request `lane`: its length, its tiles, theirs and those before it
+  // ---- the tiles of all requests, summed over the lanes: a request to each, or, of more than 64, a run of `per`
+  int kv = 0, kv0 = 0, mine = 0, ends = 0, total = 0, per = 1;  // kv: length of request kv0 + lane; ends: tiles up to a lane's
   if (ly.cut) {
-    for (int r0 = 0; r0 < a.B; r0 += 64) {
-      kv = a.kv_len[min(r0 + lane, a.B - 1)];
-      mine = r0 + lane < a.B ? request_tiles(a, pool.page_log2, kv).n : 0;
-      ends = total + wave_scan(mine);
-      total = __builtin_amdgcn_readlane(ends, 63);
+    if (a.B <= 64) {
+      kv = a.kv_len[min(lane, a.B - 1)];
+      mine = lane < a.B ? request_tiles(a, pool.page_log2, kv).n : 0;
+    } else {
+      per = (a.B + 255) / 256 * 4;
+#pragma unroll 4
+      for (int i = 0; i < per; i += 4) {
+        const int r = lane * per + i;
+        if (r + 4 <= a.B) {
+          const int4 v = *reinterpret_cast<const int4*>(a.kv_len + r);
+          mine += request_tiles(a, pool.page_log2, v.x).n + request_tiles(a, pool.page_log2, v.y).n +
+                  request_tiles(a, pool.page_log2, v.z).n + request_tiles(a, pool.page_log2, v.w).n;
+        } else {
+          for (int e = r; e < a.B; ++e) mine += request_tiles(a, pool.page_log2, a.kv_len[e]).n;
+        }
+      }
     }
+    ends = wave_scan(mine);
+    total = __builtin_amdgcn_readlane(ends, 63);
   }
   const int columns = ly.columns, sub = WIDE ? wave : 0;
   const int id = WIDE ? blockIdx.x : blockIdx.x * kWaves + wave;
@@ -174,23 +187,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
     const long long first = (long long)x * share;
     if (first < total) {
       left = min(share, total - (int)first);
-      for (int r0 = 0;; r0 += 64) {
-        if (a.B > 64) {
-          kv = a.kv_len[min(r0 + lane, a.B - 1)];
-          mine = r0 + lane < a.B ? request_tiles(a, pool.page_log2, kv).n : 0;
-          ends = before + wave_scan(mine);
-        }
+      const int l = __ffsll(__ballot(ends > (int)first)) - 1;
+      b = l * per;
+      before = __builtin_amdgcn_readlane(ends - mine, l);
+      while (per > 1) {  // which one of the run
+        kv0 = b;
+        kv = a.kv_len[min(kv0 + lane, a.B - 1)];
+        mine = kv0 + lane < a.B ? request_tiles(a, pool.page_log2, kv).n : 0;
+        ends = before + wave_scan(mine);
         const unsigned long long beyond = __ballot(ends > (int)first);
         if (beyond) {
-          const int l = __ffsll(beyond) - 1;
-          b = r0 + l;
-          before = __builtin_amdgcn_readlane(ends - mine, l);
-          kv = __builtin_amdgcn_readlane(kv, l);
-          at = (int)first - before;
+          b = kv0 + __ffsll(beyond) - 1;
+          before = __builtin_amdgcn_readlane(ends - mine, b - kv0);
           break;
         }
         before = __builtin_amdgcn_readlane(ends, 63);
+        b += 64;
       }
+      at = (int)first - before;
     }
   }
 
@@ -198,31 +212,96 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
   const bool by_request = ly.cut && ly.joined == a.B, tells = ly.cut && head_id == 0 && sub == 0 && lane == 0;
   const float sc = a.scale * a.k_scale * kLog2e;
   int2 join = make_int2(0, 0);  // of the column
-  if (!ly.cut) kv = a.kv_len[b];
-  while (left > 0) {
-    const Tiles t = request_tiles(a, pool.page_log2, __builtin_amdgcn_readfirstlane(kv));
-    const int here = min(t.n - at, left);
-    if (here <= 0) {  // no tiles
-      if (!ly.cut || ++b == a.B) break;
-      kv = a.kv_len[b];
-      at = 0;
-      continue;
-    }
+  if (!ly.cut) {
+    kv0 = b;
+    kv = a.kv_len[min(b + lane, a.B - 1)];
+  }
 
-    // ---- queries: column n of block `qt` is query head h0 + 16 qt + n (the last one again where the group ends)
-    bf16x8 q[QT][kSteps];
+  // ---- A wave's tiles in their order.  It goes through them in one pipeline, from a request to the next without a pause: the
+  // pages of a tile are asked for two tiles ahead, its rows one.  (One that ran dry at each request's end took 52.5 us instead
+  // of 49.8 for 8 requests of 8192 tokens, 8 x 128; rows two tiles ahead gained nothing anywhere.)
+  struct Place {  // the i-th of the `here` tiles that the column takes of request b, from its tile `at` on; left: with what follows
+    int b, at, here, i, left;
+    Tiles t;
+  };
+  struct Spot {  // first token of a tile, and which are visible
+    int base, lo, hi;
+  };
+  auto settle = [&](Place& p) {  // to request p.b, or the next one that has tiles; here = 0 behind the last
+    p.here = 0;
+    p.i = sub;
+    while (p.left > 0 && p.b < a.B) {
+      if (p.b - kv0 >= 64) {
+        kv0 = p.b;
+        kv = a.kv_len[min(p.b + lane, a.B - 1)];
+        asm volatile("" : "+v"(kv));  // waited for here, not on the path without it, where rows are in flight
+      }
+      p.t = request_tiles(a, pool.page_log2, __builtin_amdgcn_readlane(kv, p.b - kv0));
+      p.here = max(min(p.t.n - p.at, p.left), 0);
+      if (p.here > 0 || !ly.cut) return;
+      ++p.b;
+      p.at = 0;
+    }
+  };
+  auto after = [&](Place p) {
+    p.i += kWays;
+    if (p.i >= p.here) {
+      p.left = ly.cut ? p.left - p.here : 0;
+      ++p.b;
+      p.at = 0;
+      settle(p);
+    }
+    return p;
+  };
+  auto spot = [&](const Place& p) {  // (where a wave of a wide workgroup has no tile of a request, nothing is visible)
+    if (p.i >= p.here) return Spot{0, 0, 0};
+    const int tile = p.at + p.i;
+    return tile < p.t.n_pin ? Spot{tile * kTile, 0, p.t.pin} : Spot{p.t.base + (tile - p.t.n_pin) * kTile, p.t.lo, p.t.len};
+  };
+  // addresses: lane group g reads tokens 8 g .. 8 g + 7 of a tile, which lie on one page
+  const long long head = kvh * pool.ld_head;
+  const char* Kl = pool.K + head + (n / R::kLanes) * pool.ld_token + (n % R::kLanes) * 16;
+  const char* Vl = pool.V + head + n * (R::kRow / 16);
+  char* k_in = lds + wave * (kTile * R::kPitch) + (g * 8 + n / R::kLanes) * R::kPitch + (n % R::kLanes) * 16;
+  const char* k_out = lds + wave * (kTile * R::kPitch) + ((n >> 2) * 8 + (n & 3)) * R::kPitch + g * R::kPiece;
+  const int mask = (1 << pool.page_log2) - 1;
+  auto page_of = [&](const Place& p, const Spot& s) {
+    return a.table[min(p.b, a.B - 1) * a.ld_table + min((s.base + g * 8) >> pool.page_log2, a.max_pages - 1)];
+  };
+  auto seen = [&](const Spot& s, int page) {  // is any of this lane's eight tokens visible, on a page of the pool?
+    return page >= 0 && page < pool.n_pages && s.base + g * 8 + 7 >= s.lo && s.base + g * 8 < s.hi;
+  };
+  // Where this lane's rows lie.  Rows that are not seen are the pool's first: one line for all lanes, and loads on every path, in
+  // one order (K, page, V), let the compiler wait for just the ones it needs.
+  auto offset = [&](const Spot& s, int page) {
+    page = max(min(page, pool.n_pages - 1), 0);
+    return page * pool.ld_page + ((s.base + g * 8) & mask) * pool.ld_token;
+  };
+  auto load_k = [&](R& raw, const char* from) {
+#pragma unroll
+    for (int i = 0; i < 2 * R::kK; ++i) raw.k[i] = load<kOnce, u32x4>(from + i * R::kStep * pool.ld_token);
+  };
+  auto load_v = [&](R& raw, const char* from) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) load_words<kOnce>(from + j * pool.ld_token, raw.v[j]);
+  };
+  // queries: column n of block `qt` is query head h0 + 16 qt + n (the last one again where the group ends)
+  bf16x8 q[QT][kSteps];
+  auto load_q = [&](int request) {
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
       const int hq = min(group * 16 * QT + qt * 16 + n, G - 1);
-      const char* qp = static_cast<const char*>(a.Q) + b * a.ld_q + ((long long)kvh * G + hq) * (D * 2);
+      const char* qp = static_cast<const char*>(a.Q) + request * a.ld_q + ((long long)kvh * G + hq) * (D * 2);
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
         const int d = KV8 ? g * (D / 4) + s * 8 : (s >> 1) * 64 + g * 16 + (s & 1) * 8;
         q[qt][s] = *reinterpret_cast<const bf16x8*>(qp + d * 2);
       }
     }
-    f32x4 o[QT][kBlocks];
-    float m[QT], l[QT];
+  };
+  f32x4 o[QT][kBlocks];
+  float m[QT], l[QT];
+  auto clear = [&] {
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
       m[qt] = kNoMax;
@@ -230,54 +309,27 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
 #pragma unroll
       for (int i = 0; i < kBlocks; ++i) o[qt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+  };
 
-    // ---- addresses: lane group g reads tokens 8 g .. 8 g + 7 of a tile, which lie on one page
-    const int* row = a.table + b * a.ld_table;
-    const long long head = kvh * pool.ld_head;
-    const char* Kl = pool.K + head + (n / R::kLanes) * pool.ld_token + (n % R::kLanes) * 16;
-    const char* Vl = pool.V + head + n * (R::kRow / 16);
-    char* k_in = lds + wave * (kTile * R::kPitch) + (g * 8 + n / R::kLanes) * R::kPitch + (n % R::kLanes) * 16;
-    const char* k_out = lds + wave * (kTile * R::kPitch) + ((n >> 2) * 8 + (n & 3)) * R::kPitch + g * R::kPiece;
-    const int mask = (1 << pool.page_log2) - 1;
-    auto tile_base = [&](int i) { return i < t.n_pin ? i * kTile : t.base + (i - t.n_pin) * kTile; };
-    auto nth = [&](int i) { return min(at + i, at + here - 1); };
-    auto page_of = [&](int base) { return row[min((base + g * 8) >> pool.page_log2, a.max_pages - 1)]; };
-    // is any of this lane's eight tokens of tile i visible, on a page of the pool?
-    auto seen = [&](int i, int base, int page) {
-      const int first = base + g * 8;
-      return page >= 0 && page < pool.n_pages && first + 7 >= (i < t.n_pin ? 0 : t.lo) && first < (i < t.n_pin ? t.pin : t.len);
-    };
-    // Where this lane's rows lie.  Rows that are not seen, and those behind the last tile, are the pool's first: one line for
-    // all, and loads on every path, in one order, let the compiler wait for just the ones it needs.
-    auto offset = [&](int base, int page) {
-      page = max(min(page, pool.n_pages - 1), 0);
-      return page * pool.ld_page + ((base + g * 8) & mask) * pool.ld_token;
-    };
-    auto load_k = [&](R& raw, const char* from) {
-#pragma unroll
-      for (int i = 0; i < 2 * R::kK; ++i) raw.k[i] = load<kOnce, u32x4>(from + i * R::kStep * pool.ld_token);
-    };
-    auto load_v = [&](R& raw, const char* from) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) load_words<kOnce>(from + j * pool.ld_token, raw.v[j]);
-    };
-
-    // A tile's page is asked for two tiles ahead, its rows one, always in the order K, page, V: the wait for K then leaves V in
-    // flight.  (Rows two tiles ahead gained nothing anywhere.)
+  Place p0{b, at, 0, 0, left, {}};
+  settle(p0);
+  if (p0.here > 0) {
+    Place p1 = after(p0);
+    Spot s0 = spot(p0), s1 = spot(p1);
     R raw;
-    int tile = nth(sub), base = tile_base(tile), tile1 = nth(sub + kWays), base1 = tile_base(tile1);
-    int page = page_of(base);
-    bool ok = seen(tile, base, page);
-    const long long from = offset(base, page);
-    page = page_of(base1);
+    int page = page_of(p0, s0);
+    load_q(p0.b);
+    clear();
+    bool ok = seen(s0, page);
+    const long long from = offset(s0, page);
+    page = page_of(p1, s1);
     __builtin_amdgcn_sched_barrier(0);
-    load_k(raw, ok && sub < here ? Kl + from : pool.K);
+    load_k(raw, ok ? Kl + from : pool.K);
     __builtin_amdgcn_sched_barrier(0);
-    load_v(raw, ok && sub < here ? Vl + from : pool.V);
+    load_v(raw, ok ? Vl + from : pool.V);
     __builtin_amdgcn_sched_barrier(0);
 
-    for (int i = sub; i < here; i += kWays) {
-      const bool more = i + kWays < here;
+    while (true) {
       // ---- S^T = K Q^T
       wave_sync();
 #pragma unroll
@@ -305,20 +357,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
             s[qt][tk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[e], q[qt][e], s[qt][tk], 0, 0, 0);
         }
       }
-      const long long next = offset(base1, page);
-      const bool next_ok = seen(tile1, base1, page), there = next_ok && more;
-      const int tile2 = nth(i + 2 * kWays), base2 = tile_base(tile2);
-      load_k(raw, there ? Kl + next : pool.K);
-      page = page_of(base2);
+      const Place p2 = after(p1);
+      const Spot s2 = spot(p2);
+      const long long next = offset(s1, page);
+      const bool next_ok = seen(s1, page);
+      load_k(raw, next_ok ? Kl + next : pool.K);
+      page = page_of(p2, s2);
+      const bool last = p0.i + kWays >= p0.here;  // of this wave's tiles of the request
+      if (last) load_q(min(p1.b, a.B - 1));
 
       // ---- what is not visible: s(tk, r) belongs to token base + 8 g + 4 tk + r, V's row j to base + 8 g + j
-      const bool pinned = tile < t.n_pin;
-      const int lo = pinned ? 0 : t.lo, hi = pinned ? t.pin : t.len;
-      if (base < lo || hi - base < kTile || __ballot(!ok)) {
+      if (s0.base < s0.lo || s0.hi - s0.base < kTile || __ballot(!ok)) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int token = base + g * 8 + j;
-          const bool visible = ok && token >= lo && token < hi;
+          const int token = s0.base + g * 8 + j;
+          const bool visible = ok && token >= s0.lo && token < s0.hi;
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt) s[qt][j >> 2][j & 3] = visible ? s[qt][j >> 2][j & 3] : -__builtin_inff();
 #pragma unroll
@@ -379,119 +432,122 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
           o[qt][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, lo_w[qt], o[qt][k], 0, 0, 0);
         }
       }
-      load_v(raw, there ? Vl + next : pool.V);
-      tile = tile1;
-      base = base1;
-      tile1 = tile2;
-      base1 = base2;
+      load_v(raw, next_ok ? Vl + next : pool.V);
+
+      if (last) {
+        // ---- out: lane (g, n) holds query n's elements (4 g + r) * kBlocks + k.  The waves of a wide workgroup leave what they
+        // have in LDS, and wave r adds up the elements of its r.
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+          l[qt] += __shfl_xor(l[qt], 16);
+          l[qt] += __shfl_xor(l[qt], 32);
+        }
+        const bool whole = p0.at == 0 && p0.here == p0.t.n;
+        const long long slot = 2ll * x + (p0.at == 0 ? 1 : 0);
+        if constexpr (WIDE) {
+          __syncthreads();  // no wave has K in LDS any more
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+              for (int k = 0; k < kBlocks; k += 4)
+                part[wave][qt][r][k >> 2][lane] = f32x4{o[qt][k][r], o[qt][k + 1][r], o[qt][k + 2][r], o[qt][k + 3][r]};
+            if (g == 0) part_stat[wave][qt][n] = make_float2(m[qt], l[qt]);
+          }
+          __syncthreads();
+        }
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+          const int hq = group * 16 * QT + qt * 16 + n;
+          const long long h = (long long)kvh * G + hq;
+          float top = m[qt], sum = l[qt];
+          float weight[kWays];
+          if constexpr (WIDE) {
+            top = kNoMax;
+            sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWays; ++w) top = fmaxf(top, part_stat[w][qt][n].x);
+#pragma unroll
+            for (int w = 0; w < kWays; ++w) {
+              weight[w] = __builtin_amdgcn_exp2f(part_stat[w][qt][n].x - top);
+              sum += part_stat[w][qt][n].y * weight[w];
+            }
+          }
+          if (hq >= G) continue;
+          const float inv = !whole ? 1.f : (sum == 0.f ? 0.f : a.v_scale / sum);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            f32x4 y[kBlocks / 4];
+            int elements = (g * 4 + r) * kBlocks;
+            if constexpr (WIDE) {
+              if (r > 0) break;  // (this wave's r is its number)
+              elements = (g * 4 + wave) * kBlocks;
+#pragma unroll
+              for (int k = 0; k < kBlocks / 4; ++k) {
+                y[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < kWays; ++w) y[k] += part[w][qt][wave][k][lane] * weight[w];
+              }
+            } else {
+#pragma unroll
+              for (int k = 0; k < kBlocks / 4; ++k)
+                y[k] = f32x4{o[qt][4 * k][r], o[qt][4 * k + 1][r], o[qt][4 * k + 2][r], o[qt][4 * k + 3][r]};
+            }
+#pragma unroll
+            for (int k = 0; k < kBlocks / 4; ++k) y[k] *= inv;
+            if (!whole || out_bytes == 4) {
+              char* to = whole ? static_cast<char*>(a.O) + p0.b * a.ld_o + (h * D + elements) * 4
+                               : reinterpret_cast<char*>(ly.partial + (slot * a.N + h) * D + elements);
+#pragma unroll
+              for (int k = 0; k < kBlocks / 4; ++k) reinterpret_cast<f32x4*>(to)[k] = y[k];
+            } else {
+              char* to = static_cast<char*>(a.O) + p0.b * a.ld_o + (h * D + elements) * 2;
+              unsigned w[kBlocks / 2];
+#pragma unroll
+              for (int k = 0; k < kBlocks; k += 2) {
+                bf16x2 pair;
+                pair[0] = (__bf16)y[k >> 2][k & 3];
+                pair[1] = (__bf16)y[k >> 2][(k & 3) + 1];
+                w[k >> 1] = __builtin_bit_cast(unsigned, pair);
+              }
+              if constexpr (kBlocks == 8) *reinterpret_cast<u32x4*>(to) = u32x4{w[0], w[1], w[2], w[3]};
+              else *reinterpret_cast<u32x2*>(to) = u32x2{w[0], w[1]};
+            }
+          }
+          if (!whole && g == 0 && sub == 0) ly.stat[slot * a.N + h] = make_float2(top, sum);
+        }
+        if (ly.cut && p0.at == 0) {
+          const int spans = whole ? 0 : (before + p0.t.n - 1) / share - x + 1;
+          if (spans) join = make_int2(p0.b, spans);
+          if (by_request && tells) ly.joins[p0.b] = make_int2(x, spans);
+        }
+        before += p0.t.n;
+        if (p1.here == 0) break;
+        clear();
+        if constexpr (WIDE) __syncthreads();  // the sums are formed: K may come again
+      }
+      p0 = p1;
+      s0 = s1;
+      p1 = p2;
+      s1 = s2;
       ok = next_ok;
     }
-
-    // ---- out: lane (g, n) holds query n's elements (4 g + r) * kBlocks + k.  The waves of a wide workgroup leave what they
-    // have in LDS, and wave r adds up the elements of its r.
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-      l[qt] += __shfl_xor(l[qt], 16);
-      l[qt] += __shfl_xor(l[qt], 32);
-    }
-    const bool whole = at == 0 && here == t.n;
-    const long long slot = 2ll * x + (at == 0 ? 1 : 0);
-    if constexpr (WIDE) {
-      __syncthreads();  // no wave has K in LDS any more
-#pragma unroll
-      for (int qt = 0; qt < QT; ++qt) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int k = 0; k < kBlocks; k += 4)
-            part[wave][qt][r][k >> 2][lane] = f32x4{o[qt][k][r], o[qt][k + 1][r], o[qt][k + 2][r], o[qt][k + 3][r]};
-        if (g == 0) part_stat[wave][qt][n] = make_float2(m[qt], l[qt]);
-      }
-      __syncthreads();
-    }
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-      const int hq = group * 16 * QT + qt * 16 + n;
-      const long long h = (long long)kvh * G + hq;
-      float top = m[qt], sum = l[qt];
-      float weight[kWays];
-      if constexpr (WIDE) {
-        top = kNoMax;
-        sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWays; ++w) top = fmaxf(top, part_stat[w][qt][n].x);
-#pragma unroll
-        for (int w = 0; w < kWays; ++w) {
-          weight[w] = __builtin_amdgcn_exp2f(part_stat[w][qt][n].x - top);
-          sum += part_stat[w][qt][n].y * weight[w];
-        }
-      }
-      if (hq >= G) continue;
-      const float inv = !whole ? 1.f : (sum == 0.f ? 0.f : a.v_scale / sum);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        f32x4 y[kBlocks / 4];
-        int elements = (g * 4 + r) * kBlocks;
-        if constexpr (WIDE) {
-          if (r > 0) break;  // (this wave's r is its number)
-          elements = (g * 4 + wave) * kBlocks;
-#pragma unroll
-          for (int k = 0; k < kBlocks / 4; ++k) {
-            y[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int w = 0; w < kWays; ++w) y[k] += part[w][qt][wave][k][lane] * weight[w];
-          }
-        } else {
-#pragma unroll
-          for (int k = 0; k < kBlocks / 4; ++k)
-            y[k] = f32x4{o[qt][4 * k][r], o[qt][4 * k + 1][r], o[qt][4 * k + 2][r], o[qt][4 * k + 3][r]};
-        }
-#pragma unroll
-        for (int k = 0; k < kBlocks / 4; ++k) y[k] *= inv;
-        if (!whole || out_bytes == 4) {
-          char* to = whole ? static_cast<char*>(a.O) + b * a.ld_o + (h * D + elements) * 4
-                           : reinterpret_cast<char*>(ly.partial + (slot * a.N + h) * D + elements);
-#pragma unroll
-          for (int k = 0; k < kBlocks / 4; ++k) reinterpret_cast<f32x4*>(to)[k] = y[k];
-        } else {
-          char* to = static_cast<char*>(a.O) + b * a.ld_o + (h * D + elements) * 2;
-          unsigned w[kBlocks / 2];
-#pragma unroll
-          for (int k = 0; k < kBlocks; k += 2) {
-            bf16x2 pair;
-            pair[0] = (__bf16)y[k >> 2][k & 3];
-            pair[1] = (__bf16)y[k >> 2][(k & 3) + 1];
-            w[k >> 1] = __builtin_bit_cast(unsigned, pair);
-          }
-          if constexpr (kBlocks == 8) *reinterpret_cast<u32x4*>(to) = u32x4{w[0], w[1], w[2], w[3]};
-          else *reinterpret_cast<u32x2*>(to) = u32x2{w[0], w[1]};
-        }
-      }
-      if (!whole && g == 0 && sub == 0) ly.stat[slot * a.N + h] = make_float2(top, sum);
-    }
-    if (!ly.cut) break;
-    if (at == 0) {
-      const int spans = here < t.n ? (before + t.n - 1) / share - x + 1 : 0;
-      if (spans) join = make_int2(b, spans);
-      if (by_request && tells) ly.joins[b] = make_int2(x, spans);
-    }
-    left -= here;
-    before += t.n;
-    at = 0;
-    if (left <= 0 || ++b == a.B) break;
-    if constexpr (WIDE) __syncthreads();  // the sums are formed: K may come again
-    kv = a.kv_len[b];
   }
   if (tells && !by_request) ly.joins[x] = join;
 
-  // ---- requests without tiles
-  for (int r = x; r < a.B; r += columns) {
-    if (request_tiles(a, pool.page_log2, a.kv_len[r]).n > 0) continue;
-    const int h0 = kvh * G + group * 16 * QT, rows = min(16 * QT, G - group * 16 * QT);
-    char* to = static_cast<char*>(a.O) + r * a.ld_o + (long long)h0 * D * out_bytes;
-    if (sub == 0)
-      for (int i = lane; i < rows * D * out_bytes / 16; i += 64) reinterpret_cast<u32x4*>(to)[i] = u32x4{0, 0, 0, 0};
-    if (by_request && tells) ly.joins[r] = make_int2(0, 0);
+  // ---- requests without tiles: every columns-th from x on, looked through 64 at once
+  for (int r0 = x; r0 < a.B; r0 += 64 * columns) {
+    const long long mine_too = r0 + (long long)lane * columns;
+    const bool empty = mine_too < a.B && request_tiles(a, pool.page_log2, a.kv_len[min(mine_too, a.B - 1ll)]).n == 0;
+    for (unsigned long long todo = __ballot(empty); todo; todo &= todo - 1) {
+      const int r = r0 + (__ffsll(todo) - 1) * columns;
+      const int h0 = kvh * G + group * 16 * QT, bytes = min(16 * QT, G - group * 16 * QT) * D * out_bytes;
+      char* to = static_cast<char*>(a.O) + r * a.ld_o + (long long)h0 * D * out_bytes;
+      if (sub == 0)
+        for (int i = lane * 16; i < bytes; i += 64 * 16) *reinterpret_cast<u32x4*>(to + i) = u32x4{0, 0, 0, 0};
+      if (by_request && tells) ly.joins[r] = make_int2(0, 0);
+    }
   }
 }
 
