@@ -239,18 +239,30 @@ __global__ __launch_bounds__(kTableThreads) void paged_tables_kernel(PagedTables
   }
 }
 
-// Rows of K and V to their slots, 8 elements (16 bytes) of each per thread and turn, as bf16 or as E4M3 codes.
+// Rows of K and V to their slots, 8 elements (16 bytes) of each per thread and turn, as bf16 or as E4M3 codes.  Bound by
+// HBM.  With STREAM both sides bypass the caches: 65537 rows of 8 x 128 103.7 -> 99.5 us (5.3 TB/s; a large copy 5.2), to
+// codes 76 -> 73; but 8000 rows, which the caches hold, 13.2 -> 14.5.
 struct AppendShape {
-  int rows, chunks, head_log2;  // 8-element chunks of a row, log2 of those of a head
-  int step_r, step_c;           // the grid's stride in rows and chunks
+  unsigned rows, chunks, head_log2;  // 8-element chunks of a row, log2 of those of a head
+  unsigned step_r, step_c;           // the grid's stride in rows and chunks
   long long ld_in;
 };
-template <bool CODES>
+template <bool STREAM>
+__device__ __forceinline__ u32x4 load_row(const char* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+  return *reinterpret_cast<const u32x4*>(p);
+}
+template <bool STREAM, typename T>
+__device__ __forceinline__ void store_row(char* p, T x) {
+  if constexpr (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<T*>(p));
+  else *reinterpret_cast<T*>(p) = x;
+}
+template <bool CODES, bool STREAM>
 __global__ __launch_bounds__(256) void paged_append_kernel(const char* __restrict__ K, const char* __restrict__ V,
                                                            const int* __restrict__ slots, AppendShape a, PagedPool pool,
                                                            float inv_k, float inv_v) {
   const unsigned i = blockIdx.x * 256u + threadIdx.x;
-  int r = i / (unsigned)a.chunks, c = i - (unsigned)r * a.chunks;
+  unsigned r = i / a.chunks, c = i - r * a.chunks;
   while (r < a.rows) {
     const int slot = slots[r];
     const int page = slot >> pool.page_log2;
@@ -258,7 +270,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const char* __restric
       const long long src = r * a.ld_in + c * 16ll;
       const long long dst = page * pool.ld_page + (slot & ((1 << pool.page_log2) - 1)) * pool.ld_token +
                             (c >> a.head_log2) * pool.ld_head + (c & ((1 << a.head_log2) - 1)) * (CODES ? 8ll : 16ll);
-      const u32x4 in[2] = {*reinterpret_cast<const u32x4*>(K + src), *reinterpret_cast<const u32x4*>(V + src)};
+      const u32x4 in[2] = {load_row<STREAM>(K + src), load_row<STREAM>(V + src)};
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         char* to = const_cast<char*>(x ? pool.V : pool.K) + dst;
@@ -266,9 +278,9 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const char* __restric
           const unsigned words[4] = {in[x][0], in[x][1], in[x][2], in[x][3]};
           unsigned codes[2];
           e4m3_codes8(words, x ? inv_v : inv_k, codes);
-          *reinterpret_cast<u32x2*>(to) = u32x2{codes[0], codes[1]};
+          store_row<STREAM>(to, u32x2{codes[0], codes[1]});
         } else {
-          *reinterpret_cast<u32x4*>(to) = in[x];
+          store_row<STREAM>(to, in[x]);
         }
       }
     }
@@ -286,6 +298,11 @@ int launch_paged_tables(hipStream_t st, const PagedTables& t, bool take_pages) {
   const long long most = 4ll * compute_units();
   blocks = blocks < 1 ? 1 : (blocks > most ? most : blocks);
   const size_t lds = (size_t)(t.B + 4) / 4 * 16 * (take_pages ? 2 : 1);
+  // (sums of many requests and the waves' own pass 64 KiB together)
+  static LdsLimit limit[2];
+  const int rc = take_pages ? set_lds_limit(limit[1], paged_tables_kernel<true>, 96 << 10)
+                            : set_lds_limit(limit[0], paged_tables_kernel<false>, 96 << 10);
+  if (rc) return rc;
   if (take_pages)
     hipLaunchKernelGGL(paged_tables_kernel<true>, dim3((unsigned)blocks), dim3(kTableThreads), lds, st, t);
   else
@@ -296,21 +313,22 @@ int launch_paged_tables(hipStream_t st, const PagedTables& t, bool take_pages) {
 int launch_paged_append(hipStream_t st, const void* K, const void* V, long long ld_in_bytes, int rows, const int* slots,
                         int N, int D, const PagedPool& pool, int kv_dtype, int k_scale_log2, int v_scale_log2) {
   AppendShape a;
-  a.rows = rows;
-  a.chunks = N * D / 8;
+  a.rows = (unsigned)rows;
+  a.chunks = (unsigned)(N * D / 8);
   a.head_log2 = D == 128 ? 4 : 3;
   a.ld_in = ld_in_bytes;
   long long blocks = ((long long)rows * a.chunks + 255) / 256;
-  const long long most = 16ll * compute_units();
+  const long long most = 256ll * compute_units();
   if (blocks > most) blocks = most;
-  a.step_r = (int)(blocks * 256 / a.chunks);
-  a.step_c = (int)(blocks * 256 % a.chunks);
-  const auto k = static_cast<const char*>(K), v = static_cast<const char*>(V);
-  if (kv_dtype == PAFU_FP8_E4M3)
-    hipLaunchKernelGGL(paged_append_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, st, k, v, slots, a, pool,
-                       ldexpf(1.0f, -k_scale_log2), ldexpf(1.0f, -v_scale_log2));
-  else
-    hipLaunchKernelGGL(paged_append_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st, k, v, slots, a, pool, 1.f, 1.f);
+  a.step_r = (unsigned)(blocks * 256 / a.chunks);
+  a.step_c = (unsigned)(blocks * 256 % a.chunks);
+  const bool codes = kv_dtype == PAFU_FP8_E4M3;
+  // past the caches from 64 MiB of rows on (measured better from 128 MiB, worse up to 32)
+  const bool stream = (long long)rows * N * D * 4 >= 64ll << 20;
+  const auto kernel = codes ? (stream ? paged_append_kernel<true, true> : paged_append_kernel<true, false>)
+                            : (stream ? paged_append_kernel<false, true> : paged_append_kernel<false, false>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const char*>(K), static_cast<const char*>(V),
+                     slots, a, pool, codes ? ldexpf(1.0f, -k_scale_log2) : 1.f, codes ? ldexpf(1.0f, -v_scale_log2) : 1.f);
   return check_launch();
 }
 

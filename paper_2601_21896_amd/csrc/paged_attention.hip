@@ -181,8 +181,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
   // ---- this column's tiles: request b from its tile `at` on, `left` tiles
   int b = x, at = 0, left = 0x7fffffff, share = 0, before = 0;  // before: tiles of the requests in front of b
   if (ly.cut) {
-    share = (total + columns - 1) / columns;
-    if (WIDE && share < kWays) share = kWays;
+    share = max(total - 1, 0) / columns + 1;
+    if (WIDE && share < kWays) share = kWays;  // a tile for each wave
     left = 0;
     const long long first = (long long)x * share;
     if (first < total) {
@@ -210,7 +210,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
 
   // joins are told by request, or by column with the request in the first place
   const bool by_request = ly.cut && ly.joined == a.B, tells = ly.cut && head_id == 0 && sub == 0 && lane == 0;
-  const float sc = a.scale * a.k_scale * kLog2e;
+  const float sc = fmaxf(a.scale * a.k_scale * kLog2e, 1.1754944e-38f);  // not 0: what is not visible is -infinity times it
   int2 join = make_int2(0, 0);  // of the column
   if (!ly.cut) {
     kv0 = b;

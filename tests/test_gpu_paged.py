@@ -28,7 +28,7 @@ def bf16_values(rng, *shape):
 def _tables(kv, new, n_free, page, columns, max_slots, start, extra_ld=0, seed=0):
     rng = np.random.default_rng(seed)
     n = len(kv)
-    pages = rng.permutation(100000)[:n * columns + n_free]
+    pages = rng.permutation(max(100000, n * columns + n_free))[:n * columns + n_free]
     free, table = pages[:n_free], pages[n_free:].reshape(n, columns)
     wide = np.full((n, columns + extra_ld), -77)
     wide[:, :columns] = table
@@ -48,7 +48,7 @@ def _tables(kv, new, n_free, page, columns, max_slots, start, extra_ld=0, seed=0
 @pytest.mark.parametrize("n,page,new_high,max_extra,start,short", [
     (1, 16, 1, 0, None, 0), (1, 8, 3000, 5, 0, 0), (3, 64, 1, 3, 2, 0), (64, 16, 1, 0, 1, 0), (65, 16, 40, 7, 4, 0),
     (257, 32, 300, 1, 9, 0), (300, 8, 100, -400, 0, 60), (1000, 256, 3, 2000, 3, 10), (2, 4096, 9000, 0, 1, 1),
-    (1025, 16, 65, 0, 0, 0)])
+    (1025, 16, 65, 0, 0, 0), (8192, 8, 20, 3, 5, 100)])
 def test_tables_are_the_oracles(n, page, new_high, max_extra, start, short):
     rng = np.random.default_rng(n * 1000 + page)
     kv = rng.integers(0, 700, n) * (rng.random(n) < 0.8)
@@ -86,7 +86,7 @@ def test_tables_saturate_and_leave_tokens_past_the_limit_without_a_slot():
 
 
 @pytest.mark.parametrize("n,page,columns,extra", [(1, 16, 1, 0), (1, 64, 512, 3), (7, 8, 9, 100), (300, 16, 40, 0),
-                                                  (1500, 32, 5, -333)])
+                                                  (1500, 32, 5, -333), (8192, 8, 3, 1)])
 def test_slots_are_the_oracles(n, page, columns, extra):
     rng = np.random.default_rng(n + columns)
     table = rng.permutation(n * columns).reshape(n, columns)
@@ -309,6 +309,13 @@ def test_attention_many_short_requests_and_few_long_ones():
     _attend(list(rng.integers(0, 40, 700)), 8, 2, 64, 16, out=torch.float32)
     _attend(list(rng.integers(1, 300, 257)), 4, 4, 128, 8, out=BF)
     _attend([3, 20000, 1, 9, 0, 7000], 4, 1, 64, 64, out=torch.float32)
+
+
+def test_attention_of_the_largest_batch():
+    rng = np.random.default_rng(9)
+    lens = rng.integers(0, 30, 8192)
+    lens[4000:4090], lens[5000] = 0, 3000        # many without a token, one long
+    _attend(list(lens), 2, 2, 64, 8, out=torch.float32)
 
 
 def _plain_pool(rng, n_pages, page, kv_heads, D):
