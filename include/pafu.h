@@ -281,7 +281,7 @@ int pafu_paged_append(void* stream, const void* K, const void* V, long long ld_i
  *               long requests are cut along the token axis and joined in a second pass.  Its contents need not be
  *               initialised and are not kept.
  * Products are formed from the bf16 (or widened 8-bit) values exactly and summed in fp32; the softmax weights enter the
- * second product as the sum of two bf16 numbers (2^-17 off at most), so the result is that of fp32 arithmetic.
+ * second product as the sum of two bf16 numbers (2^-16 off at most), so an fp32 result has about 16 bits.
  * Results do not depend on timing; where requests are cut depends on the lengths in the call, which moves the last
  * bits of an fp32 result.
  */

@@ -3,15 +3,23 @@
 //
 //   O[b,h] = sum_j w_j v[j] / sum_j w_j,   w_j = 2^(s_j - m),   s_j = scale * log2(e) * q[b,h] . k[j]
 //
-// The tokens of a request are taken in tiles of 32, a wave works on a tile alone.  It forms S^T = K Q^T (16 query heads of the group as columns), the weights, and O^T += V^T W^T, all on 16x16x32 matrix
-// instructions.  The rows of the two S^T blocks of a tile are dealt to tokens so that a lane's eight weights are those
-// of eight neighbouring tokens, 8 g .. 8 g + 7 for lane group g, which is the operand layout of the second product: the
-// weights never leave their lane.  V is read by rows, a lane its 8 (or 4) neighbouring elements of its group's eight
-// tokens, and transposed within the lane by byte permutes; column n of block i is element 8 n + i.  O^T has the queries
-// in columns like S^T, so that a raise of the softmax reference is a multiplication in the lane.
+// The tokens of a request are taken in tiles of 32, a wave works on a tile alone.  It forms S^T = K Q^T (16 query heads that
+// share a key head as columns), the weights, and O^T += V^T W^T, all on 16x16x32 matrix instructions.  The rows of the two
+// S^T blocks of a tile are dealt to tokens so that a lane's eight weights are those of eight neighbouring tokens,
+// 8 g .. 8 g + 7 for lane group g, which is the operand layout of the second product: the weights never leave their lane.
+// V is read by rows, a lane its 8 (or 4) neighbouring elements of its group's eight tokens, and transposed within the lane
+// by byte permutes; column n of block i is element 8 n + i.  O^T has the queries in columns like S^T, so that a raise of
+// the softmax reference is a multiplication in the lane.
 //
-// Bound by the reads of K and V.  Every product is exact in fp32; a weight goes into the second product as the sum of
-// two bf16 numbers (one alone, 2^-9 off, would cost more than the rounding of a bf16 result).
+// Bound by the reads of K and V, at up to 6.85 TB/s (a kernel that only reads reaches 7.0; a large copy 5.2).  They bypass the
+// caches where one wave alone reads them: 6.2 TB/s otherwise.  Eight waves per compute unit, all of the launch at once, hold
+// enough rows in flight; twelve or sixteen were slower everywhere (more, shorter runs).  What a call takes beyond the reads:
+// about 5 us until the first rows are there, 7 us for the join and the way to it.
+//
+// Products of bf16 or widened 8-bit values are exact in fp32.  A weight goes into the second product as the sum of two bf16
+// numbers: its upper half, and the one nearest to what is left (less than 2^-7 of it, in steps of 2^-15: 2^-16 off at
+// most).  (One alone, 2^-8 off, would add to a bf16 result about what its own rounding does, and the matrix instructions
+// have time for both.)
 #include "pafu_internal.h"
 
 namespace pafu {
@@ -28,7 +36,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoMax = -3.0e38f;   // softmax reference before the first visible token
 constexpr float kRaiseAt = 8.f;      // weights up to 2^8: the reference is raised when a score passes it by more
 constexpr int kTile = 32;            // tokens
-constexpr int kWaves = 4;           // per workgroup
+constexpr int kWaves = 4;            // per workgroup
 constexpr int kMinShare = 4;         // tiles of a column at least where requests are cut
 constexpr int kLong = 16;            // tiles from which a request is worth a workgroup
 
@@ -404,9 +412,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
           l[qt] += w0 + w1;
           const unsigned u0 = __float_as_uint(w0), u1 = __float_as_uint(w1);
           upper[j >> 1] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);  // the upper halves
+          // What is left, and 2^-23 of the weight: greater than 0 even where nothing is, since 0 times an infinite value is none.
           bf16x2 rest;
-          rest[0] = (__bf16)(w0 - __uint_as_float(u0 & 0xffff0000u));
-          rest[1] = (__bf16)(w1 - __uint_as_float(u1 & 0xffff0000u));
+          rest[0] = (__bf16)fmaf(w0, 1.f + 0x1p-23f, -__uint_as_float(u0 & 0xffff0000u));
+          rest[1] = (__bf16)fmaf(w1, 1.f + 0x1p-23f, -__uint_as_float(u1 & 0xffff0000u));
           lower[j >> 1] = __builtin_bit_cast(unsigned, rest);
         }
         hi_w[qt] = __builtin_bit_cast(bf16x8, upper);

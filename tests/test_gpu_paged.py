@@ -179,8 +179,9 @@ def _tolerance(Q, K, V, out, n_tokens, D, scale):
     S = max(float((np.abs(K[:, h // G]) @ np.abs(Q[h])).max()) for h in range(Q.shape[0])) * scale
     # scores: D exact products summed in fp32 and scaled (each step half a unit, 2^-24, of at most S) -> D + 4 steps;
     # a weight is off by that relatively, and so is the sum of weights: twice.  The sums over tokens: n + 16 steps each.
-    # A weight enters the second product as two bf16 numbers: 2^-17.  exp2 and the division: 8 steps.
-    rel = 2 * (D + 4) * 2.0 ** -24 * S + 2 * (n_tokens + 16) * 2.0 ** -24 + 2.0 ** -17 + 8 * 2.0 ** -24
+    # A weight in [1, 2) enters the second product as its upper half and a bf16 number for the rest, which is less than 2^-7
+    # and has steps of 2^-15 at most: half a step is 2^-16.  exp2 and the division: 8 steps.
+    rel = 2 * (D + 4) * 2.0 ** -24 * S + 2 * (n_tokens + 16) * 2.0 ** -24 + 2.0 ** -16 + 8 * 2.0 ** -24
     return rel * float(np.abs(V).max()) + (2.0 ** -8 * float(np.abs(V).max()) if out == BF else 0.0)
 
 
@@ -345,6 +346,12 @@ def test_attention_infinities_and_nan_in_sight():
         assert bool(torch.isnan(got[1, :, 5]).all()) and bool((got[1, :, 6] == -math.inf).all())
         assert bool(torch.isnan(got[2]).all())
         assert bool((got[3] == 0).all())
+    # one token, whose weight is 1 to the last bit
+    Vp[7, 0, 0, 9], Vp[7, 0, 0, 10] = math.inf, -math.inf
+    for ws in (None, _ws(1, 2, 1, D)):
+        B.pafu_paged_attention(Q[:1], Kp, Vp, ints([[7, 7]]), ints([1]), O[:1], workspace=ws)
+        assert bool((O[0, :, 9] == math.inf).all()) and bool((O[0, :, 10] == -math.inf).all())
+        assert bool(torch.isfinite(O[0, :, :9]).all())
 
 
 def test_attention_on_a_side_stream_and_twice_with_one_result():
