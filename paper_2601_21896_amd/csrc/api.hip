@@ -930,8 +930,8 @@ int pafu_paged_attention(void* stream, const void* Q, long long ld_q, const void
   rc = check_paged_lists(B, page_size, max_pages, ld_table, 0, log2);
   if (rc) return rc;
   if (N < 1 || N > (1 << 16) - 1 || N % N_kv != 0 || n_pinned < 0 || window < 0) return PAFU_ERR_SHAPE;
-  // the tiles of all requests are counted in 32 bits
-  if (B > 0 && ((((long long)max_pages << pool.page_log2) + 31) / 32) > 0x7fffffffll / B) return PAFU_ERR_SHAPE;
+  const long long row_tokens = (long long)max_pages << pool.page_log2, max_tokens = row_tokens < 0x7fffffff ? row_tokens : 0x7fffffff;
+  if (B > 0 && (max_tokens + 31) / 32 > 0x7fffffffll / B) return PAFU_ERR_SHAPE;  // the tiles of all requests: 32 bits
   const int ob = dtype_bytes(out_dtype);
   if (ob == 0) return PAFU_ERR_DTYPE;
   const long long row = (long long)N * D;
@@ -950,7 +950,8 @@ int pafu_paged_attention(void* stream, const void* Q, long long ld_q, const void
   if (any_overlap(outs, ins)) return PAFU_ERR_ALIAS;
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)D);
   const bool kv8 = kv_dtype == PAFU_FP8_E4M3;
-  const PagedAttention a{Q, O, block_table, kv_len, ld_q * 2, ld_o * ob, ld_table, B, N, N_kv, D, max_pages, n_pinned, window,
+  const PagedAttention a{Q, O, block_table, kv_len, ld_q * 2, ld_o * ob, ld_table, B, N, N_kv, D, max_pages, (int)max_tokens,
+                         n_pinned, window,
                          kv_dtype, out_dtype, scale, kv8 ? ldexpf(1.0f, k_scale_log2) : 1.0f,
                          kv8 ? ldexpf(1.0f, v_scale_log2) : 1.0f};
   return launch_paged_attention(static_cast<hipStream_t>(stream), a, pool, workspace, workspace_bytes);

@@ -164,7 +164,7 @@ struct PagedAttention {
   void* O;
   const int *table, *kv_len;
   long long ld_q, ld_o, ld_table;  // ld_q, ld_o in bytes
-  int B, N, N_kv, D, max_pages, n_pinned, window, kv_dtype, out_dtype;
+  int B, N, N_kv, D, max_pages, max_tokens, n_pinned, window, kv_dtype, out_dtype;  // max_tokens: of a row of the table
   float scale, k_scale, v_scale;
 };
 size_t paged_attention_workspace_bytes(int B, int N, int N_kv, int D);

@@ -60,10 +60,9 @@ struct Tiles {
   int pin, lo, len, base;  // base: first token of the first tile of [lo, len)
 };
 __device__ __forceinline__ int tiles_of(int tokens) { return tokens > 0 ? (tokens - 1) / kTile + 1 : 0; }
-__device__ __forceinline__ Tiles request_tiles(const PagedAttention& a, int page_log2, int kv_len) {
+__device__ __forceinline__ Tiles request_tiles(const PagedAttention& a, int kv_len) {
   Tiles t;
-  const long long most = (long long)a.max_pages << page_log2;
-  t.len = kv_len < 0 ? 0 : (kv_len < most ? kv_len : (int)most);
+  t.len = min(max(kv_len, 0), a.max_tokens);
   t.lo = 0;
   t.pin = 0;
   if (a.window > 0 && kv_len > a.window) {
@@ -162,7 +161,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
   if (ly.cut) {
     if (a.B <= 64) {
       kv = a.kv_len[min(lane, a.B - 1)];
-      mine = lane < a.B ? request_tiles(a, pool.page_log2, kv).n : 0;
+      mine = lane < a.B ? request_tiles(a, kv).n : 0;
     } else {
       per = (a.B + 255) / 256 * 4;
 #pragma unroll 4
@@ -170,10 +169,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
         const int r = lane * per + i;
         if (r + 4 <= a.B) {
           const int4 v = *reinterpret_cast<const int4*>(a.kv_len + r);
-          mine += request_tiles(a, pool.page_log2, v.x).n + request_tiles(a, pool.page_log2, v.y).n +
-                  request_tiles(a, pool.page_log2, v.z).n + request_tiles(a, pool.page_log2, v.w).n;
+          mine += request_tiles(a, v.x).n + request_tiles(a, v.y).n +
+                  request_tiles(a, v.z).n + request_tiles(a, v.w).n;
         } else {
-          for (int e = r; e < a.B; ++e) mine += request_tiles(a, pool.page_log2, a.kv_len[e]).n;
+          for (int e = r; e < a.B; ++e) mine += request_tiles(a, a.kv_len[e]).n;
         }
       }
     }
@@ -201,7 +200,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
       while (per > 1) {  // which one of the run
         kv0 = b;
         kv = a.kv_len[min(kv0 + lane, a.B - 1)];
-        mine = kv0 + lane < a.B ? request_tiles(a, pool.page_log2, kv).n : 0;
+        mine = kv0 + lane < a.B ? request_tiles(a, kv).n : 0;
         ends = before + wave_scan(mine);
         const unsigned long long beyond = __ballot(ends > (int)first);
         if (beyond) {
@@ -244,7 +243,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
         kv = a.kv_len[min(p.b + lane, a.B - 1)];
         asm volatile("" : "+v"(kv));  // waited for here, not on the path without it, where rows are in flight
       }
-      p.t = request_tiles(a, pool.page_log2, __builtin_amdgcn_readlane(kv, p.b - kv0));
+      p.t = request_tiles(a, __builtin_amdgcn_readlane(kv, p.b - kv0));
       p.here = max(min(p.t.n - p.at, p.left), 0);
       if (p.here > 0 || !ly.cut) return;
       ++p.b;
@@ -548,7 +547,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
   // ---- requests without tiles: every columns-th from x on, looked through 64 at once
   for (int r0 = x; r0 < a.B; r0 += 64 * columns) {
     const long long mine_too = r0 + (long long)lane * columns;
-    const bool empty = mine_too < a.B && request_tiles(a, pool.page_log2, a.kv_len[min(mine_too, a.B - 1ll)]).n == 0;
+    const bool empty = mine_too < a.B && request_tiles(a, a.kv_len[min(mine_too, a.B - 1ll)]).n == 0;
     for (unsigned long long todo = __ballot(empty); todo; todo &= todo - 1) {
       const int r = r0 + (__ffsll(todo) - 1) * columns;
       const int h0 = kvh * G + group * 16 * QT, bytes = min(16 * QT, G - group * 16 * QT) * D * out_bytes;
@@ -693,7 +692,7 @@ int launch_paged_attention(hipStream_t st, const PagedAttention& a, const PagedP
   Layout ly;
   ly.groups = query_groups(a.N, a.N_kv, a.D).groups;
   ly.heads = a.N_kv * ly.groups;
-  const long long longest = ((((long long)a.max_pages << pool.page_log2) + kTile - 1) / kTile);
+  const long long longest = ((long long)a.max_tokens + kTile - 1) / kTile;
   ly.cut = workspace != nullptr && workspace_bytes >= paged_attention_workspace_bytes(a.B, a.N, a.N_kv, a.D) &&
            longest > kMinShare;
   ly.columns = a.B;
