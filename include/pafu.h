@@ -278,8 +278,9 @@ int pafu_paged_append(void* stream, const void* K, const void* V, long long ld_i
  *                                        any size
  *   workspace : optional (NULL / 0 allowed).  With pafu_paged_attention_workspace_bytes(B, N, N_kv, D) bytes (16-byte
  *               aligned, apart from every tensor of the call) the tokens of all requests are shared out evenly over the GPU:
- *               long requests are cut along the token axis and joined in a second pass.  Its contents need not be
- *               initialised and are not kept.
+ *               long requests are cut along the token axis and joined in a second pass; not where the table is too narrow
+ *               for more than 512 tokens (max_pages should not be larger than the batch needs).  Its contents need not
+ *               be initialised and are not kept.
  * Products are formed from the bf16 (or widened 8-bit) values exactly and summed in fp32; the softmax weights enter the
  * second product as the sum of two bf16 numbers (2^-16 off at most), so an fp32 result has about 16 bits.
  * Results do not depend on timing; where requests are cut depends on the lengths in the call, which moves the last

@@ -37,8 +37,6 @@ constexpr float kNoMax = -3.0e38f;   // softmax reference before the first visib
 constexpr float kRaiseAt = 8.f;      // weights up to 2^8: the reference is raised when a score passes it by more
 constexpr int kTile = 32;            // tokens
 constexpr int kWaves = 4;            // per workgroup
-constexpr int kMinShare = 4;         // tiles of a column at least where requests are cut
-constexpr int kLong = 16;            // tiles from which a request is worth a workgroup
 
 // How the work is laid out.  A column is a run of tiles of the requests' concatenated tile lists, or, where nothing is cut, a
 // request.  Every (key head, group of query heads) of a column is one wave, neighbouring heads are one workgroup
@@ -692,9 +690,16 @@ int launch_paged_attention(hipStream_t st, const PagedAttention& a, const PagedP
   Layout ly;
   ly.groups = query_groups(a.N, a.N_kv, a.D).groups;
   ly.heads = a.N_kv * ly.groups;
-  const long long longest = ((long long)a.max_tokens + kTile - 1) / kTile;
+  const long long longest = ((long long)a.max_tokens + kTile - 1) / kTile, items = (long long)a.B * ly.heads;
+  const int units = compute_units();
+  // Short requests are not cut: the join and the way to it (7 us) cost more than an even share is worth.  By the most tiles that
+  // a request may have, cut -> whole: 8 tiles, 100 requests of 150 .. 250 tokens, 32 / 8 heads of 128, 26.5 -> 18.9 us; 16
+  // tiles, 256 of 300 .. 512 86 -> 73 us, 400 of 100 .. 500 with one key head 27 -> 18; 32 tiles, 4 of 300 .. 1000 11.5 -> 17.4.
+  // With more than 512 waves (two workgroups to a unit) and less than 2048 (all that fit) the longest ones decide: 16 tiles, 128
+  // of 100 .. 512 with 12 / 12 heads 40 -> 51.
+  const bool one_round = ly.heads >= kWaves && items > 2 * units && items < 8 * units;
   ly.cut = workspace != nullptr && workspace_bytes >= paged_attention_workspace_bytes(a.B, a.N, a.N_kv, a.D) &&
-           longest > kMinShare;
+           longest > (one_round ? 8 : 16);
   ly.columns = a.B;
   ly.joined = 0;
   ly.partial = nullptr;
@@ -702,8 +707,7 @@ int launch_paged_attention(hipStream_t st, const PagedAttention& a, const PagedP
   ly.joins = nullptr;
   // Cut: wide where a workgroup's four heads would not be neighbours in memory.  Whole: wide where the requests may be long, or
   // where the launch has few waves.
-  const bool wide = ly.cut ? ly.heads < kWaves || pool.ld_head > pool.ld_token
-                           : longest >= kLong || (long long)a.B * ly.heads <= 2ll * compute_units();
+  const bool wide = ly.cut ? ly.heads < kWaves || pool.ld_head > pool.ld_token : longest > 16 || items <= 2 * units;
   if (ly.cut) {
     const size_t all = (size_t)cut_columns(ly.heads, false);
     const long long useful = longest * a.B, most = cut_columns(ly.heads, wide);

@@ -256,8 +256,9 @@ def _attend(lens, heads, kv_heads, D, page, kv="bf16", layout="token", out=BF, p
 @pytest.mark.parametrize("kv", ["bf16", "e4m3"])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("heads,kv_heads", [(1, 1), (4, 1), (12, 12), (32, 8), (35, 5), (48, 2), (17, 1), (64, 1)])
-def test_attention_head_layouts(heads, kv_heads, D, kv, out):
-    _attend([0, 1, 33, 300, 77], heads, kv_heads, D, 16, kv=kv, out=out, seed=heads * D)
+@pytest.mark.parametrize("columns", [None, 64], ids=["narrow table", "wide table"])   # (a wide one lets requests be cut)
+def test_attention_head_layouts(heads, kv_heads, D, kv, out, columns):
+    _attend([0, 1, 33, 300, 77], heads, kv_heads, D, 16, kv=kv, out=out, seed=heads * D, columns=columns)
 
 
 @pytest.mark.parametrize("ws", [True, False], ids=["cut", "whole"])
@@ -271,8 +272,10 @@ def test_attention_lengths_and_page_sizes(lens, page, ws):
 @pytest.mark.parametrize("kv", ["bf16", "e4m3"])
 @pytest.mark.parametrize("layout", LAYOUTS)
 def test_attention_pool_layouts(layout, kv):
-    _attend([70, 5, 0, 450], 6, 3, 128, 16, kv=kv, layout=layout, out=torch.float32, extra_ld=3)
-    _attend([70, 5, 0, 450], 6, 1, 64, 32, kv=kv, layout=layout, out=torch.float32)
+    for columns in (None, 100):
+        _attend([70, 5, 0, 450], 6, 3, 128, 16, kv=kv, layout=layout, out=torch.float32, extra_ld=3, columns=columns)
+        _attend([70, 5, 0, 450], 20, 5, 128, 16, kv=kv, layout=layout, out=torch.float32, columns=columns)
+        _attend([70, 5, 0, 450], 6, 1, 64, 32, kv=kv, layout=layout, out=torch.float32, columns=columns)
 
 
 @pytest.mark.parametrize("window,pinned", [(1, 0), (1, 1), (5, 0), (64, 3), (100, 33), (33, 100), (1000, 7), (5000, 0),
@@ -290,6 +293,7 @@ def test_attention_pages_outside_the_pool_take_no_part():
         table[3, 0:4] = -5
     for kv in ("bf16", "e4m3"):
         _attend([200, 50, 17, 65], 8, 4, 128, 16, kv=kv, out=torch.float32, spoil=spoil)
+        _attend([200, 50, 17, 65], 8, 4, 128, 16, kv=kv, out=torch.float32, spoil=spoil, columns=80)
         _attend([2000, 50, 17, 650], 8, 4, 64, 16, kv=kv, out=torch.float32, spoil=spoil)
 
 
@@ -308,6 +312,9 @@ def test_attention_scores_far_apart(kv):
 def test_attention_many_short_requests_and_few_long_ones():
     rng = np.random.default_rng(5)
     _attend(list(rng.integers(0, 40, 700)), 8, 2, 64, 16, out=torch.float32)
+    _attend(list(rng.integers(0, 40, 700)), 8, 2, 64, 16, out=torch.float32, columns=40)
+    _attend(list(rng.integers(0, 40, 300)), 16, 8, 128, 16, out=torch.float32, columns=40)
+    _attend(list(rng.integers(300, 512, 130)), 8, 8, 64, 16, out=torch.float32)
     _attend(list(rng.integers(1, 300, 257)), 4, 4, 128, 8, out=BF)
     _attend([3, 20000, 1, 9, 0, 7000], 4, 1, 64, 64, out=torch.float32)
 
@@ -316,6 +323,8 @@ def test_attention_of_the_largest_batch():
     rng = np.random.default_rng(9)
     lens = rng.integers(0, 30, 8192)
     lens[4000:4090], lens[5000] = 0, 3000        # many without a token, one long
+    _attend(list(lens), 2, 2, 64, 8, out=torch.float32)
+    lens[5000] = 30
     _attend(list(lens), 2, 2, 64, 8, out=torch.float32)
 
 
