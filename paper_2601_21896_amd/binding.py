@@ -1,4 +1,4 @@
-"""ctypes binding of libpafu.so: argument marshalling only.
+"""Binding of libpafu.so: argument marshalling only, with ctypes (the paged calls: in C++, csrc/paged_call.cpp).
 
 Every function here has the name and the argument order of its C entry point in
 include/pafu.h; tensors are torch CUDA(HIP) tensors whose data pointers are handed
@@ -437,115 +437,57 @@ def pafu_sse_score(Q, K, block_len, out, workspace, softmax_scale=0.0, stream=No
     return out
 
 
-# ---- paged K/V cache.  Lengths, tables and slots are read on the device, so what the C side cannot see of them (their
-# type, size and device) is checked here.
+# ---- paged K/V cache.  A decode step makes these calls for every layer, so their arguments are marshalled in C++
+# (csrc/paged_call.cpp): a third of what ctypes takes.  It also checks what the C side cannot see of lists that are read on
+# the device: TypeError for a wrong type, ValueError for a wrong shape, stride or place (all tensors have to be on the current
+# GPU).
 
-def _paged_stream(stream, *tensors):
-    """The stream of a call whose tensors (None: not given) all lie on the current device."""
-    import torch
-    device = tensors[0].get_device()
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError("the tensors are on different devices")
-    if device < 0:
-        raise ValueError("the tensors must be on the GPU")
-    if device != torch.cuda.current_device():
-        raise ValueError("the tensors are on GPU %d and the current device is %d" % (device, torch.cuda.current_device()))
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
+_PAGED = None  # (the library whose entry points the module holds, the module)
 
 
-def _int32_list(name, t, n=None):
-    import torch
-    shape = t.shape
-    if t.dtype is not torch.int32:
-        raise TypeError("%s must be int32, not %s" % (name, t.dtype))
-    if len(shape) != 1 or not t.is_contiguous() or (n is not None and shape[0] != n):
-        raise ValueError("%s must be a contiguous list%s, not %s with strides %s"
-                         % (name, "" if n is None else " of %d" % n, tuple(shape), t.stride()))
-    return t.data_ptr()
+def _paged():
+    global _PAGED
+    lib = _lib()
+    if _PAGED is None or _PAGED[0] is not lib:
+        import torch
+        try:
+            from . import _paged_call as call
+        except ImportError as e:
+            raise RuntimeError("_paged_call.so is not built for this Python and torch (%s); run `python -c 'import "
+                               "__graft_entry__ as g; g.build()'`" % e) from e
+        if call.torch_version != torch.__version__.split("+")[0]:
+            raise RuntimeError("_paged_call.so was built with torch %s, this is %s: build again"
+                               % (call.torch_version, torch.__version__))
+        call.bind(*(ctypes.cast(f, c_void_p).value for f in (lib.pafu_paged_tables, lib.pafu_paged_slots,
+                                                             lib.pafu_paged_append, lib.pafu_paged_attention)),
+                  torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+        _PAGED = lib, call
+    return _PAGED[1]
 
 
-def _block_table(t, n):
-    import torch
-    shape, strides = t.shape, t.stride()
-    if t.dtype is not torch.int32:
-        raise TypeError("the block table must be int32, not %s" % t.dtype)
-    if len(shape) != 2 or shape[0] != n or (shape[1] > 1 and strides[1] != 1):
-        raise ValueError("the block table must be [%d, max_pages] with contiguous rows, not %s with strides %s"
-                         % (n, tuple(shape), strides))
-    return t.data_ptr(), shape[1], strides[0] if n > 1 else max(shape[1], 1)
-
-
-def _pool_dtype(K_pages, V_pages):
-    """dtype code of a page pool after the checks that need its shape: both tensors alike, elements contiguous."""
-    import torch
-    shape, strides, dtype = K_pages.shape, K_pages.stride(), K_pages.dtype
-    if len(shape) != 4 or V_pages.shape != shape or V_pages.stride() != strides or strides[3] != 1:
-        raise ValueError("the page tensors must be [n_pages, page_size, N_kv, D] of one shape and stride, elements contiguous")
-    if V_pages.dtype is dtype:
-        if dtype is torch.bfloat16:
-            return PAFU_BF16
-        if dtype is torch.uint8:
-            return PAFU_FP8_E4M3
-    raise TypeError("page tensors are bfloat16 or uint8 (E4M3 codes), not %s and %s" % (dtype, V_pages.dtype))
-
-
-def _rows_3d(name, t, dtypes):
-    """[rows, heads, D] with contiguous rows of one of `dtypes` -> token stride."""
-    shape, strides = t.shape, t.stride()
-    if t.dtype not in dtypes:
-        raise TypeError("%s has the unsupported dtype %s" % (name, t.dtype))
-    if len(shape) != 3:
-        raise ValueError("%s must be [rows, heads, D], not %s" % (name, tuple(shape)))
-    rows, heads, D = shape
-    if (D > 1 and strides[2] != 1) or (heads > 1 and strides[1] != D):
-        raise ValueError("%s must have contiguous rows, not strides %s" % (name, strides))
-    return strides[0] if rows > 1 else heads * D
+def _given(stream):
+    return stream if stream is None or isinstance(stream, int) else stream.cuda_stream
 
 
 def pafu_paged_tables(kv_len, new_len, free_pages, page_size, block_table, slots, row_start, kv_len_out, free_end,
                       free_start=None, stream=None):
     """Pages from free_pages for every request's new tokens, entered in block_table [B, max_pages], and their slots."""
-    B = kv_len.shape[0]
-    st = _paged_stream(stream, kv_len, new_len, free_pages, block_table, slots, row_start, kv_len_out, free_end, free_start)
-    table, max_pages, ld_table = _block_table(block_table, B)
-    rc = _lib().pafu_paged_tables(st, _int32_list("kv_len", kv_len), _int32_list("new_len", new_len, B), B,
-                                  _int32_list("free_pages", free_pages), free_pages.shape[0],
-                                  None if free_start is None else _int32_list("free_start", free_start, 1), page_size,
-                                  table, max_pages, ld_table, _int32_list("slots", slots), slots.shape[0],
-                                  _int32_list("row_start", row_start, B + 1), _int32_list("kv_len_out", kv_len_out, B),
-                                  _int32_list("free_end", free_end, 1))
+    rc = _paged().tables(kv_len, new_len, free_pages, page_size, block_table, slots, row_start, kv_len_out, free_end,
+                         free_start, _given(stream))
     _check(rc, "pafu_paged_tables")
     return slots
 
 
 def pafu_paged_slots(block_table, start, count, page_size, slots, row_start, stream=None):
     """Slots of the tokens start[b] .. start[b] + count[b] - 1 of every request, request after request."""
-    B = start.shape[0]
-    st = _paged_stream(stream, block_table, start, count, slots, row_start)
-    table, max_pages, ld_table = _block_table(block_table, B)
-    rc = _lib().pafu_paged_slots(st, table, max_pages, ld_table, _int32_list("start", start),
-                                 _int32_list("count", count, B), B, page_size, _int32_list("slots", slots), slots.shape[0],
-                                 _int32_list("row_start", row_start, B + 1))
-    _check(rc, "pafu_paged_slots")
+    _check(_paged().slots(block_table, start, count, page_size, slots, row_start, _given(stream)), "pafu_paged_slots")
     return slots
 
 
 def pafu_paged_append(K, V, slots, K_pages, V_pages, k_scale_log2=0, v_scale_log2=0, stream=None):
     """K, V: [rows, N, D] bf16 -> K_pages, V_pages: [n_pages, page_size, N, D] bf16, or uint8 E4M3 codes of value /
     2^scale_log2, at the rows' slots (int32; a slot outside the pool leaves its row out)."""
-    import torch
-    st = _paged_stream(stream, K, V, slots, K_pages, V_pages)
-    kv_dtype = _pool_dtype(K_pages, V_pages)
-    n_pages, page_size, N, D = K_pages.shape
-    ld_in = _rows_3d("K", K, (torch.bfloat16,))
-    rows = K.shape[0]
-    if K.shape[1] != N or K.shape[2] != D or V.shape != K.shape or _rows_3d("V", V, (torch.bfloat16,)) != ld_in:
-        raise ValueError("K and V must be [rows, %d, %d] with one stride, not %s and %s" % (N, D, tuple(K.shape), tuple(V.shape)))
-    ld = K_pages.stride()
-    rc = _lib().pafu_paged_append(st, K.data_ptr(), V.data_ptr(), ld_in, rows, _int32_list("slots", slots, rows),
-                                  N, D, K_pages.data_ptr(), V_pages.data_ptr(), n_pages, page_size, ld[0], ld[1], ld[2],
-                                  kv_dtype, k_scale_log2, v_scale_log2)
+    rc = _paged().append(K, V, slots, K_pages, V_pages, k_scale_log2, v_scale_log2, _given(stream))
     _check(rc, "pafu_paged_append")
     return K_pages, V_pages
 
@@ -557,26 +499,7 @@ def pafu_paged_attention_workspace_bytes(B: int, N: int, N_kv: int, D: int) -> i
 def pafu_paged_attention(Q, K_pages, V_pages, block_table, kv_len, O, n_pinned=0, window=0, softmax_scale=0.0,
                          k_scale_log2=0, v_scale_log2=0, workspace=None, stream=None):
     """Q, O: [B, N, D], one new token per request; K_pages, V_pages: [n_pages, page_size, N_kv, D] bf16 or uint8 codes."""
-    import torch
-    st = _paged_stream(stream, Q, K_pages, V_pages, block_table, kv_len, O, workspace)
-    kv_dtype = _pool_dtype(K_pages, V_pages)
-    n_pages, page_size, N_kv, D = K_pages.shape
-    ld_q, ld_o = _rows_3d("Q", Q, (torch.bfloat16,)), _rows_3d("O", O, (torch.bfloat16, torch.float32))
-    shape = Q.shape
-    B, N = shape[0], shape[1]
-    if shape[2] != D or O.shape != shape:
-        raise ValueError("Q and O must be [B, N, %d], not %s and %s" % (D, tuple(Q.shape), tuple(O.shape)))
-    table, max_pages, ld_table = _block_table(block_table, B)
-    ld = K_pages.stride()
-    ws, ws_bytes = None, 0
-    if workspace is not None:
-        if not workspace.is_contiguous():
-            raise ValueError("the workspace must be contiguous")
-        ws, ws_bytes = workspace.data_ptr(), workspace.nbytes
-    rc = _lib().pafu_paged_attention(st, Q.data_ptr(), ld_q, K_pages.data_ptr(), V_pages.data_ptr(), n_pages,
-                                     page_size, ld[0], ld[1], ld[2], kv_dtype, k_scale_log2, v_scale_log2, table, max_pages,
-                                     ld_table, _int32_list("kv_len", kv_len, B), B, N, N_kv, D, n_pinned, window,
-                                     float(softmax_scale), O.data_ptr(), ld_o,
-                                     PAFU_BF16 if O.dtype is torch.bfloat16 else PAFU_F32, ws, ws_bytes)
+    rc = _paged().attention(Q, K_pages, V_pages, block_table, kv_len, O, n_pinned, window, softmax_scale, k_scale_log2,
+                            v_scale_log2, workspace, _given(stream))
     _check(rc, "pafu_paged_attention")
     return O

@@ -1,4 +1,5 @@
-"""Builds libpafu.so (HIP kernels + C ABI) for gfx950 in-tree with hipcc."""
+"""Builds libpafu.so (HIP kernels + C ABI) for gfx950 in-tree with hipcc, and _paged_call.so, the marshalling of the paged
+calls, with the host compiler."""
 
 from __future__ import annotations
 
@@ -11,6 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpafu.so")
+CALL = os.path.join(HERE, "_paged_call.so")
 SOURCES = ["api.hip", "score.hip", "select.hip", "compact.hip", "quant.hip", "attention.hip", "sse.hip",
            "paged.hip", "paged_attention.hip"]
 FLAGS = [
@@ -39,8 +41,23 @@ def _run(cmd):
     return out
 
 
+def build_call() -> str:
+    """Compiles the Python module that hands torch tensors to the paged calls (no GPU code)."""
+    import sysconfig
+
+    import torch
+    torch_dir = os.path.dirname(torch.__file__)
+    include, lib_dir = os.path.join(torch_dir, "include"), os.path.join(torch_dir, "lib")
+    return _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+                 "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
+                 "-I", sysconfig.get_path("include"), "-isystem", include,
+                 "-isystem", os.path.join(include, "torch", "csrc", "api", "include"),
+                 "-I", os.path.join(ROOT, "include"), os.path.join(CSRC, "paged_call.cpp"), "-o", CALL,
+                 "-L", lib_dir, "-Wl,-rpath," + lib_dir, "-ltorch_python", "-ltorch_cpu", "-lc10"])
+
+
 def build(verbose: bool = False, extra_flags=(), out: str = "") -> str:
-    """Compiles every translation unit and links libpafu.so; always recompiles.
+    """Compiles every translation unit and links libpafu.so, and the Python module beside it; always recompiles.
 
     `out` names another library file next to libpafu.so (study builds with extra -D flags, loaded by name through
     bench.py --library); its objects go to a directory of their own so that the product build is left alone."""
@@ -54,7 +71,10 @@ def build(verbose: bool = False, extra_flags=(), out: str = "") -> str:
         return _run([cc, *FLAGS, *extra_flags, "-c", os.path.join(CSRC, SOURCES[i]), "-o", objs[i]])
 
     with ThreadPoolExecutor(max_workers=min(len(SOURCES), 8)) as ex:
+        call = ex.submit(build_call) if not out else None
         logs = list(ex.map(one, range(len(SOURCES))))
+        if call is not None:
+            logs.append(call.result())
     logs.append(_run([cc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]))
     if verbose:
         print("\n".join(l for l in logs if l.strip()))

@@ -94,37 +94,74 @@ def test_attention_refuses_bad_arguments():
 
 
 def test_binding_refuses_tensors_that_are_not_on_the_gpu():
-    i = torch.zeros(4, dtype=torch.int32)
+    i, more = torch.zeros(4, dtype=torch.int32), torch.zeros(5, dtype=torch.int32)
     pages = torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16)
     rows = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="GPU"):
-        B.pafu_paged_tables(i, i, i, 16, i.view(4, 1), i, i, i, i)
+        B.pafu_paged_tables(i, i, i, 16, i.view(4, 1), i, more, i, i[:1])
     with pytest.raises(ValueError, match="GPU"):
-        B.pafu_paged_slots(i.view(4, 1), i, i, 16, i, i)
+        B.pafu_paged_slots(i.view(4, 1), i, i, 16, i, more)
     with pytest.raises(ValueError, match="GPU"):
         B.pafu_paged_append(rows, rows, i, pages, pages)
     with pytest.raises(ValueError, match="GPU"):
         B.pafu_paged_attention(rows, pages, pages, i.view(4, 1), i, rows)
 
 
-def test_binding_checks_types_and_shapes_that_the_library_cannot_see():
+def test_binding_refuses_types_and_shapes_that_the_library_cannot_see():
     i = torch.zeros(6, dtype=torch.int32)
     pages = torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16)
-    for bad, error in ((i.long(), TypeError), (i[::2], ValueError), (i.view(2, 3), ValueError), (i[:3], ValueError)):
+    rows = torch.zeros(6, 2, 64, dtype=torch.bfloat16)
+    table = i.view(6, 1)
+    bad_lists = ((i.long(), TypeError), (i[::2], ValueError), (i.view(2, 3), ValueError), (i[:3], ValueError), (None, TypeError),
+                 ([0] * 6, TypeError))
+    for bad, error in bad_lists:
         with pytest.raises(error):
-            B._int32_list("list", bad, 6)
-    for bad, error in ((i.view(2, 3).long(), TypeError), (i.view(3, 2), ValueError), (i.view(3, 2).t(), ValueError), (i, ValueError)):
+            B.pafu_paged_tables(i, bad, i, 16, table, i, torch.zeros(7, dtype=torch.int32), i, i[:1])
         with pytest.raises(error):
-            B._block_table(bad, 2)
-    assert B._block_table(i.view(2, 3)[:, :2], 2)[1:] == (2, 3)
-    assert B._pool_dtype(pages, pages) == B.PAFU_BF16
-    assert B._pool_dtype(pages.view(torch.uint8), pages.view(torch.uint8)) == B.PAFU_FP8_E4M3
+            B.pafu_paged_slots(table, i, bad, 16, i, torch.zeros(7, dtype=torch.int32))
+        with pytest.raises(error):
+            B.pafu_paged_append(rows, rows, bad, pages, pages)
+        with pytest.raises(error):
+            B.pafu_paged_attention(rows, pages, pages, table, bad, rows)
+    for bad in (i, i[:5]):                                           # row_start holds one more than there are requests
+        with pytest.raises(ValueError, match="row_start"):
+            B.pafu_paged_slots(table, i, i, 16, i, bad)
+    for bad, error in ((table.long(), TypeError), (i, ValueError), (i.view(3, 2), ValueError),
+                       (torch.zeros(2, 6, dtype=torch.int32).t(), ValueError)):
+        with pytest.raises(error, match="block table"):
+            B.pafu_paged_attention(rows, pages, pages, bad, i, rows)
     for K, V, error in ((pages, pages[:1], ValueError), (pages[0], pages[0], ValueError), (pages, pages.half(), TypeError),
-                        (pages.float(), pages.float(), TypeError), (pages.transpose(2, 3), pages.transpose(2, 3), ValueError)):
+                        (pages.float(), pages.float(), TypeError), (pages.transpose(2, 3), pages.transpose(2, 3), ValueError),
+                        (pages, pages.transpose(0, 1).contiguous().transpose(0, 1), ValueError)):
+        with pytest.raises(error, match="page tensors"):
+            B.pafu_paged_attention(rows, K, V, table, i, rows)
+        with pytest.raises(error, match="page tensors"):
+            B.pafu_paged_append(rows, rows, i, K, V)
+    wide = torch.zeros(6, 4, 128, dtype=torch.bfloat16)
+    for bad, error in ((rows.half(), TypeError), (rows[0], ValueError), (wide[:, ::2, :64], ValueError), (wide[:, :2, ::2], ValueError),
+                       (rows[:, :, :32], ValueError)):
         with pytest.raises(error):
-            B._pool_dtype(K, V)
-    rows = torch.zeros(4, 3, 64, dtype=torch.bfloat16)
-    assert B._rows_3d("rows", rows[::2], (torch.bfloat16,)) == 2 * 3 * 64
-    for bad, error in ((rows.float(), TypeError), (rows[0], ValueError), (rows[:, ::2], ValueError), (rows[:, :, ::2], ValueError)):
+            B.pafu_paged_attention(bad, pages, pages, table, i, rows)
         with pytest.raises(error):
-            B._rows_3d("rows", bad, (torch.bfloat16,))
+            B.pafu_paged_append(bad, rows, i, pages, pages)
+    with pytest.raises(ValueError, match="one stride"):
+        B.pafu_paged_append(rows, wide.view(6, 8, 64)[:, :2], i, pages, pages)
+    with pytest.raises(ValueError, match="Q and O"):
+        B.pafu_paged_attention(rows, pages, pages, table, i, rows[:, :1])
+    with pytest.raises(ValueError, match="workspace"):
+        B.pafu_paged_attention(rows, pages, pages, table, i, rows, workspace=torch.zeros(8, dtype=torch.uint8)[::2])
+    with pytest.raises(OverflowError):
+        B.pafu_paged_attention(rows, pages, pages, table, i, rows, window=2 ** 31)
+    for bad in ("16", 1.5):
+        with pytest.raises(TypeError):
+            B.pafu_paged_slots(table, i, i, bad, i, torch.zeros(7, dtype=torch.int32))
+
+
+def test_the_module_takes_the_entry_points_of_the_loaded_library():
+    call = B._paged()
+    assert B._paged() is call
+    assert call.torch_version == torch.__version__.split("+")[0]
+    with pytest.raises(TypeError):
+        call.attention(1, 2)
+    with pytest.raises(TypeError):
+        call.bind(1)
