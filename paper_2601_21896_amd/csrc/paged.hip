@@ -59,7 +59,8 @@ __global__ __launch_bounds__(kTableThreads) void paged_tables_kernel(PagedTables
   extern __shared__ int lds[];
   const int stride4 = (t.B + 4) / 4 * 4;  // room for B + 1, 16-byte aligned
   int* rows = lds;
-  int* first = lds + stride4;  // (TAKE)
+  int* begin = lds + stride4;      // each request's start
+  int* first = lds + 2 * stride4;  // (TAKE)
   __shared__ int wave_rows[2][kTableWaves], wave_pages[2][kTableWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int page_mask = (1 << t.page_log2) - 1;
@@ -69,12 +70,12 @@ __global__ __launch_bounds__(kTableThreads) void paged_tables_kernel(PagedTables
     const int b0 = base + tid * 4;
     int n[4], s[4], total[4], need[4], sum_rows = 0, sum_pages = 0;
     load4(t.count, b0, t.B, n);
-    if (TAKE) load4(t.start, b0, t.B, s);
+    load4(t.start, b0, t.B, s);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       n[e] = max(n[e], 0);
+      s[e] = max(s[e], 0);
       if (TAKE) {
-        s[e] = max(s[e], 0);
         total[e] = sat_add(s[e], n[e]);
         need[e] = pages_of(total[e]) - pages_of(s[e]);
         sum_pages = sat_add(sum_pages, need[e]);
@@ -113,6 +114,7 @@ __global__ __launch_bounds__(kTableThreads) void paged_tables_kernel(PagedTables
         }
       }
       store4(rows, b0, t.B, r);
+      store4(begin, b0, t.B, s);
       if (TAKE) store4(first, b0, t.B, p);
     }
   }
@@ -163,10 +165,10 @@ __global__ __launch_bounds__(kTableThreads) void paged_tables_kernel(PagedTables
       of[e] = b;
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) slot[e] = t.start[of[e]];  // (its token 0)
+    for (int e = 0; e < 4; ++e) slot[e] = begin[of[e]];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int s = max(slot[e], 0);
+      const int s = slot[e];
       token[e] = (unsigned)s + (unsigned)(found[e] ? (int)(i0 + e) - rows[of[e]] : 0);
       const unsigned col = token[e] >> t.page_log2;
       found[e] = found[e] && col < (unsigned)t.max_pages;
@@ -199,12 +201,11 @@ __global__ __launch_bounds__(kTableThreads) void paged_tables_kernel(PagedTables
     if (TAKE) {
       int n[4], s[4], total[4], page[4], at[4];
       load4(t.count, b0, t.B, n);
-      load4(t.start, b0, t.B, s);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         at[e] = first[min(b0 + e, t.B)];
         page[e] = at[e] < t.n_free && b0 + e < t.B ? t.free_pages[at[e]] : -1;
-        s[e] = max(s[e], 0);
+        s[e] = begin[min(b0 + e, t.B - 1)];
         total[e] = sat_add(s[e], max(n[e], 0));
       }
       store4(t.kv_len_out, b0, t.B, total);
@@ -228,10 +229,10 @@ __global__ __launch_bounds__(kTableThreads) void paged_tables_kernel(PagedTables
       const int j = j0 + lane * waves, mine = j < jobs ? j % t.B : 0;
       for (unsigned long long todo = __ballot(j < jobs && first[mine + 1] - first[mine] > 1 + j / t.B * 64); todo;
            todo &= todo - 1) {
-        const int job = j0 + (__ffsll(todo) - 1) * waves, b = job % t.B, part = job / t.B, begin = first[b];
-        const int have = pages_of(max(t.start[b], 0)), in_table = min(first[b + 1] - begin, t.max_pages - have);
+        const int job = j0 + (__ffsll(todo) - 1) * waves, b = job % t.B, part = job / t.B, from = first[b];
+        const int have = pages_of(begin[b]), in_table = min(first[b + 1] - from, t.max_pages - have);
         for (int i = 1 + part * 64 + lane; i < in_table; i += parts * 64) {
-          const int at = sat_add(begin, i);
+          const int at = sat_add(from, i);
           t.table[b * t.ld_table + have + i] = at < t.n_free ? t.free_pages[at] : -1;
         }
       }
@@ -266,11 +267,19 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const char* __restric
   while (r < a.rows) {
     const int slot = slots[r];
     const int page = slot >> pool.page_log2;
+    const long long src = r * a.ld_in + c * 16ll;
+    u32x4 in[2];
+    if constexpr (!STREAM) {  // a small call is a chain of reads: the rows do not wait for their slot
+      in[0] = load_row<false>(K + src);
+      in[1] = load_row<false>(V + src);
+    }
     if (slot >= 0 && page < pool.n_pages) {
-      const long long src = r * a.ld_in + c * 16ll;
       const long long dst = page * pool.ld_page + (slot & ((1 << pool.page_log2) - 1)) * pool.ld_token +
                             (c >> a.head_log2) * pool.ld_head + (c & ((1 << a.head_log2) - 1)) * (CODES ? 8ll : 16ll);
-      const u32x4 in[2] = {load_row<STREAM>(K + src), load_row<STREAM>(V + src)};
+      if constexpr (STREAM) {
+        in[0] = load_row<true>(K + src);
+        in[1] = load_row<true>(V + src);
+      }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         char* to = const_cast<char*>(x ? pool.V : pool.K) + dst;
@@ -297,11 +306,11 @@ int launch_paged_tables(hipStream_t st, const PagedTables& t, bool take_pages) {
   long long blocks = ((long long)t.max_slots + kTableThreads * 4 - 1) / (kTableThreads * 4);
   const long long most = 4ll * compute_units();
   blocks = blocks < 1 ? 1 : (blocks > most ? most : blocks);
-  const size_t lds = (size_t)(t.B + 4) / 4 * 16 * (take_pages ? 2 : 1);
-  // (sums of many requests and the waves' own pass 64 KiB together)
+  const size_t lds = (size_t)(t.B + 4) / 4 * 16 * (take_pages ? 3 : 2);
+  // (the lists of more than 5000 requests pass 64 KiB)
   static LdsLimit limit[2];
-  const int rc = take_pages ? set_lds_limit(limit[1], paged_tables_kernel<true>, 96 << 10)
-                            : set_lds_limit(limit[0], paged_tables_kernel<false>, 96 << 10);
+  const int rc = take_pages ? set_lds_limit(limit[1], paged_tables_kernel<true>, 100 << 10)
+                            : set_lds_limit(limit[0], paged_tables_kernel<false>, 100 << 10);
   if (rc) return rc;
   if (take_pages)
     hipLaunchKernelGGL(paged_tables_kernel<true>, dim3((unsigned)blocks), dim3(kTableThreads), lds, st, t);

@@ -316,18 +316,30 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
     }
   };
 
+  // Where nothing is cut and all tokens are visible, the first pages and the queries do not wait for the length (small calls
+  // are chains of reads).
+  const bool early = !ly.cut && a.window == 0;
+  int page = 0, page1 = 0;
   Place p0{b, at, 0, 0, left, {}};
+  if (early) {
+    page = page_of(p0, Spot{sub * kTile, 0, 0});
+    page1 = page_of(p0, Spot{(sub + kWays) * kTile, 0, 0});
+    load_q(b);
+  }
   settle(p0);
   if (p0.here > 0) {
     Place p1 = after(p0);
     Spot s0 = spot(p0), s1 = spot(p1);
     R raw;
-    int page = page_of(p0, s0);
-    load_q(p0.b);
+    if (!early) {
+      page = page_of(p0, s0);
+      load_q(p0.b);
+      page1 = page_of(p1, s1);
+    }
     clear();
     bool ok = seen(s0, page);
     const long long from = offset(s0, page);
-    page = page_of(p1, s1);
+    page = page1;
     __builtin_amdgcn_sched_barrier(0);
     load_k(raw, ok ? Kl + from : pool.K);
     __builtin_amdgcn_sched_barrier(0);
