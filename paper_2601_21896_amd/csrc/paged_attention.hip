@@ -12,7 +12,7 @@
 // the softmax reference is a multiplication in the lane.
 //
 // Bound by the reads of K and V, at up to 6.85 TB/s (a kernel that only reads reaches 7.0; a large copy 5.2).  They bypass the
-// caches where one wave alone reads them: 6.2 TB/s otherwise.  Eight waves per compute unit, all of the launch at once, hold
+// caches where one wave alone reads their lines: 6.2 TB/s otherwise (where waves share lines, the caches are worth it).  Eight waves per compute unit, all of the launch at once, hold
 // enough rows in flight; twelve or sixteen were slower everywhere (more, shorter runs).  What a call takes beyond the reads:
 // about 5 us until the first rows are there, 7 us for the join and the way to it.
 //
@@ -138,11 +138,10 @@ __device__ __forceinline__ unsigned widen2(unsigned w, bool upper) {
                : __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
 }
 
-template <int D, bool KV8, int QT, bool WIDE>
+template <int D, bool KV8, int QT, bool WIDE, bool ONCE>  // ONCE: no other wave reads the same lines of K and V
 __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAttention a, PagedPool pool, Layout ly) {
   constexpr int kSteps = D / 32;   // matrix instructions of one S^T block
   constexpr int kBlocks = D / 16;  // blocks of O^T
-  constexpr bool kOnce = QT == 1;  // K and V are read by one wave only
   using R = Raw<D, KV8>;
   constexpr int kWays = WIDE ? kWaves : 1;
   // K on its way to the matrix instructions, then what the waves of a wide workgroup add up
@@ -284,11 +283,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
   };
   auto load_k = [&](R& raw, const char* from) {
 #pragma unroll
-    for (int i = 0; i < 2 * R::kK; ++i) raw.k[i] = load<kOnce, u32x4>(from + i * R::kStep * pool.ld_token);
+    for (int i = 0; i < 2 * R::kK; ++i) raw.k[i] = load<ONCE, u32x4>(from + i * R::kStep * pool.ld_token);
   };
   auto load_v = [&](R& raw, const char* from) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) load_words<kOnce>(from + j * pool.ld_token, raw.v[j]);
+    for (int j = 0; j < 8; ++j) load_words<ONCE>(from + j * pool.ld_token, raw.v[j]);
   };
   // queries: column n of block `qt` is query head h0 + 16 qt + n (the last one again where the group ends)
   bf16x8 q[QT][kSteps];
@@ -667,12 +666,12 @@ void launch_join(hipStream_t st, const PagedAttention& a, const Layout& ly) {
   if (a.out_dtype == PAFU_F32) hipLaunchKernelGGL((paged_join_kernel<D, true, SPLIT>), grid, dim3(256), 0, st, a, ly);
   else hipLaunchKernelGGL((paged_join_kernel<D, false, SPLIT>), grid, dim3(256), 0, st, a, ly);
 }
-template <int D, bool KV8, int QT>
+template <int D, bool KV8, int QT, bool ONCE>
 int launch(hipStream_t st, const PagedAttention& a, const PagedPool& pool, const Layout& ly, bool wide) {
   const long long jobs = (long long)ly.columns * ly.heads;
   const dim3 threads(64 * kWaves), blocks((unsigned)(wide ? jobs : (jobs + kWaves - 1) / kWaves));
-  if (wide) hipLaunchKernelGGL((paged_attention_kernel<D, KV8, QT, true>), blocks, threads, 0, st, a, pool, ly);
-  else hipLaunchKernelGGL((paged_attention_kernel<D, KV8, QT, false>), blocks, threads, 0, st, a, pool, ly);
+  if (wide) hipLaunchKernelGGL((paged_attention_kernel<D, KV8, QT, true, ONCE>), blocks, threads, 0, st, a, pool, ly);
+  else hipLaunchKernelGGL((paged_attention_kernel<D, KV8, QT, false, ONCE>), blocks, threads, 0, st, a, pool, ly);
   int rc = check_launch();
   if (rc || !ly.cut) return rc;
   // few requests in many columns: four workgroups to a row, which ask for four times as many partial results at once
@@ -680,12 +679,18 @@ int launch(hipStream_t st, const PagedAttention& a, const PagedPool& pool, const
   else launch_join<D, 1>(st, a, ly);
   return check_launch();
 }
+// Do the rows of neighbouring heads share the 128 bytes of a line?
+bool shared_lines(const PagedAttention& a, const PagedPool& pool) {
+  return a.D == 64 && a.kv_dtype == PAFU_FP8_E4M3 && a.N_kv > 1 && pool.ld_head < 128;
+}
 template <int D, bool KV8>
 int launch(hipStream_t st, const PagedAttention& a, const PagedPool& pool, const Layout& ly, bool wide) {
   switch (query_groups(a.N, a.N_kv, D).qt) {
-    case 1: return launch<D, KV8, 1>(st, a, pool, ly, wide);
-    case 2: return launch<D, KV8, 2>(st, a, pool, ly, wide);
-    default: return launch<64, KV8, 3>(st, a, pool, ly, wide);  // (D is 64)
+    case 1:
+      if (D == 64 && KV8 && shared_lines(a, pool)) return launch<64, true, 1, false>(st, a, pool, ly, wide);
+      return launch<D, KV8, 1, true>(st, a, pool, ly, wide);
+    case 2: return launch<D, KV8, 2, false>(st, a, pool, ly, wide);
+    default: return launch<64, KV8, 3, false>(st, a, pool, ly, wide);  // (D is 64)
   }
 }
 
@@ -717,9 +722,11 @@ int launch_paged_attention(hipStream_t st, const PagedAttention& a, const PagedP
   ly.partial = nullptr;
   ly.stat = nullptr;
   ly.joins = nullptr;
-  // Cut: wide where a workgroup's four heads would not be neighbours in memory.  Whole: wide where the requests may be long, or
-  // where the launch has few waves.
-  const bool wide = ly.cut ? ly.heads < kWaves || pool.ld_head > pool.ld_token : longest > 16 || items <= 2 * units;
+  // Cut: wide where a workgroup's four heads would not be neighbours in memory; narrow where waves share what they read, so that
+  // they do so through one compute unit's cache (48 / 1 heads of 128 202 -> 154 us; 8-bit rows of 64, 8 / 2 heads, 112 -> 72).
+  // Whole: wide where the requests may be long, or where the launch has few waves.
+  const bool wide = ly.cut ? ly.groups == 1 && ((ly.heads < kWaves && !shared_lines(a, pool)) || pool.ld_head > pool.ld_token)
+                           : longest > 16 || items <= 2 * units;
   if (ly.cut) {
     const size_t all = (size_t)cut_columns(ly.heads, false);
     const long long useful = longest * a.B, most = cut_columns(ly.heads, wide);
