@@ -12,7 +12,7 @@
 // the softmax reference is a multiplication in the lane.
 //
 // Bound by the reads of K and V, at up to 6.85 TB/s (a kernel that only reads reaches 7.0; a large copy 5.2).  They bypass the
-// caches where one wave alone reads their lines: 6.2 TB/s otherwise (where waves share lines, the caches are worth it).  Eight waves per compute unit, all of the launch at once, hold
+// caches where one wave alone reads their lines (6.2 TB/s otherwise), except in small calls.  Eight waves per compute unit, all of the launch at once, hold
 // enough rows in flight; twelve or sixteen were slower everywhere (more, shorter runs).  What a call takes beyond the reads:
 // about 5 us until the first rows are there, 7 us for the join and the way to it.
 //
@@ -683,14 +683,22 @@ int launch(hipStream_t st, const PagedAttention& a, const PagedPool& pool, const
 bool shared_lines(const PagedAttention& a, const PagedPool& pool) {
   return a.D == 64 && a.kv_dtype == PAFU_FP8_E4M3 && a.N_kv > 1 && pool.ld_head < 128;
 }
+template <int D, bool KV8, int QT>
+int launch(hipStream_t st, const PagedAttention& a, const PagedPool& pool, const Layout& ly, bool wide) {
+  // Past the caches from 16 MiB of K and V on, which is the most that the table has room for: 16 requests of 1000 tokens in 16
+  // places of memory in turn 18.2 -> 16.9 us (in three places, which the caches hold, 15.1 -> 16.4), 32 of 1000 .. 2048
+  // 42.5 -> 37.5; below, one of 4096 12.4 -> 12.8.
+  const long long seen = a.window > 0 && a.window < a.max_tokens - (long long)a.n_pinned ? (long long)a.window + a.n_pinned : a.max_tokens;
+  const bool small = seen * a.B * a.N_kv <= (16ll << 20) / (2 * D * (KV8 ? 1 : 2));
+  return ly.groups == 1 && !shared_lines(a, pool) && !small ? launch<D, KV8, QT, true>(st, a, pool, ly, wide)
+                                                            : launch<D, KV8, QT, false>(st, a, pool, ly, wide);
+}
 template <int D, bool KV8>
 int launch(hipStream_t st, const PagedAttention& a, const PagedPool& pool, const Layout& ly, bool wide) {
   switch (query_groups(a.N, a.N_kv, D).qt) {
-    case 1:
-      if (D == 64 && KV8 && shared_lines(a, pool)) return launch<64, true, 1, false>(st, a, pool, ly, wide);
-      return launch<D, KV8, 1, true>(st, a, pool, ly, wide);
-    case 2: return launch<D, KV8, 2, false>(st, a, pool, ly, wide);
-    default: return launch<64, KV8, 3, false>(st, a, pool, ly, wide);  // (D is 64)
+    case 1: return launch<D, KV8, 1>(st, a, pool, ly, wide);
+    case 2: return launch<D, KV8, 2>(st, a, pool, ly, wide);
+    default: return launch<64, KV8, 3>(st, a, pool, ly, wide);  // (D is 64)
   }
 }
 
