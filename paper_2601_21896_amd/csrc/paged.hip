@@ -56,7 +56,7 @@ __device__ __forceinline__ void store4(int* p, int at, int n, const int (&x)[4])
 // entered by the thread that summed it.
 template <bool TAKE>
 __global__ __launch_bounds__(kTableThreads) void paged_tables_kernel(PagedTables t) {
-  extern __shared__ int lds[];
+  extern __shared__ __attribute__((aligned(16))) int lds[];
   const int stride4 = (t.B + 4) / 4 * 4;  // room for B + 1, 16-byte aligned
   int* rows = lds;
   int* begin = lds + stride4;      // each request's start
