@@ -236,18 +236,18 @@ int pafu_chunk_attention_fp8(void* stream, const void* Q, int Lq, const void* Kc
 /* pafu_paged_tables - pages and slots for the tokens that each request is about to append.
  *   have(b) = ceil(kv_len[b] / page_size), want(b) = ceil((kv_len[b] + new_len[b]) / page_size)
  *   block_table[b, have(b) + i] = free_pages[at(b) + i]    0 <= i < want(b) - have(b)
- *   at(b)        = *free_start + the pages that requests before b take (free_start NULL: 0)
+ *   at(b)        = *free_start + the pages that requests before b take (free_start NULL or negative: 0)
  *   *free_end    = *free_start + the pages that all requests take: the next call's free_start
  *   row_start[b] = the new tokens of the requests before b (b = 0 .. B): the first row of request b
  *   slots[row_start[b] + j] = slot of request b's token kv_len[b] + j, 0 <= j < new_len[b]
  *   kv_len_out[b] = kv_len[b] + new_len[b]
  *   kv_len, new_len : [B]   free_pages : [n_free]   block_table : [B, max_pages], in and out, other entries unchanged
- *   slots : [max_slots]; rows behind the last one get -1, rows that do not fit are left out
+ *   slots : [max_slots], at most 2^30; rows behind the last one get -1, rows that do not fit are left out
  *   row_start : [B + 1]   kv_len_out : [B]   free_start, free_end : one int32 each (4-byte aligned)
  * A page that the list does not hold (*free_end > n_free says so) is entered as -1; one beyond max_pages is not entered
  * but counted; slots of either are -1.  Negative lengths count as 0, sums saturate at 2^31 - 1.
  * pafu_paged_slots - the same slots for tokens that have their pages: request b's tokens start[b] .. start[b] +
- * count[b] - 1.  A token whose page is negative or beyond max_pages gets -1.
+ * count[b] - 1.  A token whose page is negative or beyond max_pages, or whose slot passes 2^31 - 1, gets -1.
  */
 int pafu_paged_tables(void* stream, const int* kv_len, const int* new_len, int B, const int* free_pages, int n_free,
                       const int* free_start, int page_size, int* block_table, int max_pages, long long ld_table,
@@ -284,7 +284,8 @@ int pafu_paged_append(void* stream, const void* K, const void* V, long long ld_i
  * Products are formed from the bf16 (or widened 8-bit) values exactly and summed in fp32; the softmax weights enter the
  * second product as the sum of two bf16 numbers (2^-16 off at most), so an fp32 result has about 16 bits.
  * Results do not depend on timing; where requests are cut depends on the lengths in the call, which moves the last
- * bits of an fp32 result.
+ * bits of an fp32 result.  Calls that may overlap in time need workspaces of their own.  PAFU_ERR_SHAPE where
+ * the table's room, B * ceil(max_pages * page_size / 32), passes 2^31 - 1, or B * N does 2^24 - 1.
  */
 size_t pafu_paged_attention_workspace_bytes(int B, int N, int N_kv, int D);
 int pafu_paged_attention(void* stream, const void* Q, long long ld_q, const void* K_pages, const void* V_pages,

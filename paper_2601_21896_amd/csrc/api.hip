@@ -198,7 +198,8 @@ bool any_overlap(const Span (&outs)[N_OUT], const Span (&ins)[N_IN]) {
   return false;
 }
 int check_paged_lists(int B, int page_size, int max_pages, long long ld_table, int max_slots, int& page_log2) {
-  if (B < 0 || B > PAFU_PAGED_MAX_REQUESTS || max_pages < 1 || ld_table < max_pages || ld_table > (1ll << 40) || max_slots < 0)
+  if (B < 0 || B > PAFU_PAGED_MAX_REQUESTS || max_pages < 1 || ld_table < max_pages || ld_table > (1ll << 40) || max_slots < 0 ||
+      max_slots > (1 << 30))
     return PAFU_ERR_SHAPE;
   if (page_size < 8 || page_size > 4096 || (page_size & (page_size - 1)) != 0) return PAFU_ERR_SHAPE;
   page_log2 = 3;
@@ -932,6 +933,7 @@ int pafu_paged_attention(void* stream, const void* Q, long long ld_q, const void
   if (N < 1 || N > (1 << 16) - 1 || N % N_kv != 0 || n_pinned < 0 || window < 0) return PAFU_ERR_SHAPE;
   const long long row_tokens = (long long)max_pages << pool.page_log2, max_tokens = row_tokens < 0x7fffffff ? row_tokens : 0x7fffffff;
   if (B > 0 && (max_tokens + 31) / 32 > 0x7fffffffll / B) return PAFU_ERR_SHAPE;  // the tiles of all requests: 32 bits
+  if ((long long)B * N >= (1 << 24)) return PAFU_ERR_SHAPE;  // a launch's threads: 32 bits
   const int ob = dtype_bytes(out_dtype);
   if (ob == 0) return PAFU_ERR_DTYPE;
   const long long row = (long long)N * D;

@@ -24,7 +24,7 @@ def test_tables_refuse_bad_arguments():
         assert call(**{name: ok[name] + 4}) == -4, name
     assert call(fe=ok["fe"] + 2) == -4
     for kw in (dict(B=-1), dict(B=8193), dict(nf=-1), dict(ps=0), dict(ps=4), dict(ps=24), dict(ps=8192), dict(ps=-16),
-               dict(mp=0), dict(ld=7), dict(ms=-1)):
+               dict(mp=0), dict(ld=7), dict(ms=-1), dict(ms=2 ** 30 + 1)):
         assert call(**kw) == -2, kw
     # in place is not allowed, nor are outputs over inputs or over each other
     for kw in (dict(out=A), dict(rs=A + MB), dict(fe=A + 3 * MB), dict(slots=A + 4 * MB), dict(table=A + 2 * MB),
@@ -39,7 +39,7 @@ def test_slots_refuse_bad_arguments():
     for name in ("table", "start", "count", "slots", "rs"):
         assert call(**{name: None}) == -1, name
         assert call(**{name: ok[name] + 8}) == -4, name
-    for kw in (dict(B=-1), dict(B=8193), dict(ps=12), dict(mp=0), dict(ld=7), dict(ms=-1)):
+    for kw in (dict(B=-1), dict(B=8193), dict(ps=12), dict(mp=0), dict(ld=7), dict(ms=-1), dict(ms=2 ** 30 + 1)):
         assert call(**kw) == -2, kw
     for kw in (dict(slots=A), dict(rs=A + 2 * MB), dict(rs=A + 3 * MB)):
         assert call(**kw) == -6, kw
@@ -83,6 +83,9 @@ def test_attention_refuses_bad_arguments():
                dict(ldq=1023), dict(ldo=1000), dict(ks=65), dict(mp=0), dict(ld=7)) + BAD_POOLS:
         assert call(**kw) == -2, kw
     assert call(dt=1) == -3 and call(od=2) == -3
+    assert call(B=4096, N=4096, ldq=4096 * 128, ldo=4096 * 128) == -2  # a launch's threads are counted in 32 bits
+    # and so are the tiles of all requests
+    assert call(B=8192, mp=1 << 20, ld=1 << 20, ps=4096, ldp=4096 * 256) == -2
     for kw in (dict(ldq=1028), dict(ldo=1028), dict(ws=A + 4 * MB + 8, wsb=1024)):
         assert call(**kw) == -4, kw
     for kw in (dict(O=A), dict(O=ok["Kp"] + 4096), dict(O=A + MB), dict(ws=A, wsb=64), dict(ws=ok["Vp"], wsb=64),
