@@ -282,7 +282,8 @@ int pafu_paged_append(void* stream, const void* K, const void* V, long long ld_i
  *               for more than 512 tokens (max_pages should not be larger than the batch needs).  Its contents need not
  *               be initialised and are not kept.
  * Products are formed from the bf16 (or widened 8-bit) values exactly and summed in fp32; the softmax weights enter the
- * second product as the sum of two bf16 numbers (2^-16 off at most), so an fp32 result has about 16 bits.
+ * second product with all their 24 bits.  A weight of less than 2^-118 of the request's largest may be 0: times an infinite
+ * value it is NaN.
  * Results do not depend on timing; where requests are cut depends on the lengths in the call, which moves the last
  * bits of an fp32 result.  Calls that may overlap in time need workspaces of their own.  PAFU_ERR_SHAPE where
  * the table's room, B * ceil(max_pages * page_size / 32), passes 2^31 - 1, or B * N does 2^24 - 1.

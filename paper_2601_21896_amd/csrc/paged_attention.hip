@@ -16,10 +16,8 @@
 // enough rows in flight; twelve or sixteen were slower everywhere (more, shorter runs).  What a call takes beyond the reads:
 // about 5 us until the first rows are there, 7 us for the join and the way to it.
 //
-// Products of bf16 or widened 8-bit values are exact in fp32.  A weight goes into the second product as the sum of two bf16
-// numbers: its upper half, and the one nearest to what is left (less than 2^-7 of it, in steps of 2^-15: 2^-16 off at
-// most).  (One alone, 2^-8 off, would add to a bf16 result about what its own rounding does, and the matrix instructions
-// have time for both.)
+// Products of bf16 or widened 8-bit values are exact in fp32.  A weight goes into the second product whole: as the sum of
+// three bf16 numbers, which hold eight of its 24 bits each.
 #include "pafu_internal.h"
 
 namespace pafu {
@@ -31,6 +29,7 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoMax = -3.0e38f;   // softmax reference before the first visible token
@@ -130,6 +129,12 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// A float's upper half is a bf16 number, the float with its lower bits cut off; behind: what is cut off (exact).
+__device__ __forceinline__ float behind(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+__device__ __forceinline__ u16x2 upper_halves(float x, float y) {
+  return __builtin_bit_cast(u16x2, __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u));
 }
 
 // two codes of a word -> two bf16 (exact; the tensor's scale is applied elsewhere)
@@ -396,7 +401,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
       }
 
       // ---- weights
-      bf16x8 hi_w[QT], lo_w[QT];
+      bf16x8 w_parts[QT][3];
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
         float top = s[qt][0][0];
@@ -412,22 +417,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
 #pragma unroll
           for (int k = 0; k < kBlocks; ++k) o[qt][k] *= down;
         }
-        u32x4 upper, lower;
+        u32x4 part0, part1, part2;
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
           const float w0 = __builtin_amdgcn_exp2f(fmaf(s[qt][j >> 2][j & 3], sc, -m[qt]));
           const float w1 = __builtin_amdgcn_exp2f(fmaf(s[qt][j >> 2][(j & 3) + 1], sc, -m[qt]));
           l[qt] += w0 + w1;
-          const unsigned u0 = __float_as_uint(w0), u1 = __float_as_uint(w1);
-          upper[j >> 1] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);  // the upper halves
-          // What is left, and 2^-23 of the weight: greater than 0 even where nothing is, since 0 times an infinite value is none.
-          bf16x2 rest;
-          rest[0] = (__bf16)fmaf(w0, 1.f + 0x1p-23f, -__uint_as_float(u0 & 0xffff0000u));
-          rest[1] = (__bf16)fmaf(w1, 1.f + 0x1p-23f, -__uint_as_float(u1 & 0xffff0000u));
-          lower[j >> 1] = __builtin_bit_cast(unsigned, rest);
+          // A weight's bits eight at a time.  Where none are left, a part of a weight that is not 0 is the least bf16 number: the
+          // parts of 0 alone are 0, and 0 times an infinite value is none.
+          const float r0 = behind(w0), r1 = behind(w1);
+          const u16x2 first = upper_halves(w0, w1), least = __builtin_elementwise_min(first, u16x2{1, 1});
+          part0[j >> 1] = __builtin_bit_cast(unsigned, first);
+          part1[j >> 1] = __builtin_bit_cast(unsigned, __builtin_elementwise_max(upper_halves(r0, r1), least));
+          part2[j >> 1] = __builtin_bit_cast(unsigned, __builtin_elementwise_max(upper_halves(behind(r0), behind(r1)), least));
         }
-        hi_w[qt] = __builtin_bit_cast(bf16x8, upper);
-        lo_w[qt] = __builtin_bit_cast(bf16x8, lower);
+        w_parts[qt][0] = __builtin_bit_cast(bf16x8, part0);
+        w_parts[qt][1] = __builtin_bit_cast(bf16x8, part1);
+        w_parts[qt][2] = __builtin_bit_cast(bf16x8, part2);
       }
 
       // ---- O^T += V^T W^T: block k of this lane's elements, rows transposed in the lane
@@ -444,10 +450,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
           w[j] = __builtin_amdgcn_perm(v[2 * j + 1][k >> 1], v[2 * j][k >> 1], (k & 1) ? 0x07060302u : 0x05040100u);
         const bf16x8 vt = __builtin_bit_cast(bf16x8, w);
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt) {
-          o[qt][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, hi_w[qt], o[qt][k], 0, 0, 0);
-          o[qt][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, lo_w[qt], o[qt][k], 0, 0, 0);
-        }
+        for (int e = 0; e < 3; ++e)
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt)
+            o[qt][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w_parts[qt][e], o[qt][k], 0, 0, 0);
       }
       load_v(raw, next_ok ? Vl + next : pool.V);
 

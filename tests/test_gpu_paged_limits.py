@@ -1,0 +1,84 @@
+"""Attention of one new token at the limits of its numbers: the bits of its weights, infinities, rows that see nothing."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import pafu_oracle as orc
+from paper_2601_21896_amd import binding as B
+from tests.gpu_util import DEV
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+def ints(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(DEV)
+
+
+def _codes(x):
+    """Pages as they are stored: bf16 values, or the E4M3 codes of x (scale 1)."""
+    return torch.from_numpy(orc.quantise_e4m3(x.double().numpy(), 0)).to(DEV)
+
+
+def _workspace(n, heads, kv_heads, D):
+    """The bytes of a call's workspace, filled with 0xa5."""
+    size = B.pafu_paged_attention_workspace_bytes(n, heads, kv_heads, D)
+    return torch.full((size,), 0xA5, dtype=torch.uint8, device=DEV)
+
+
+@pytest.mark.parametrize("columns", [8, 80], ids=["whole", "cut"])   # (room for more than 512 tokens: cut)
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads,kv_heads,D", [(16, 1, 128), (8, 4, 128), (32, 1, 128), (16, 4, 64), (48, 1, 64)])
+def test_attention_weights_keep_their_24_bits(heads, kv_heads, D, kv, columns):
+    # Values are rows of the identity, token j's is 1 at element j: the result is the softmax itself.  Scores are one exact
+    # product each, q0 * k0, of at most 4 in steps that bf16 and E4M3 hold.
+    n, tokens, page = 6, 64, 16
+    rng = np.random.default_rng(heads + D)
+    K, V = torch.zeros(n, columns * page, kv_heads, D), torch.zeros(n, columns * page, kv_heads, D)
+    k0 = rng.integers(-8, 9, (n, tokens, kv_heads)) / 8.0               # 4 bits: E4M3 numbers
+    q0 = rng.integers(-255, 256, (n, heads)) / 64.0                     # 8 bits: bf16 numbers
+    K[:, :tokens, :, 0] = torch.from_numpy(k0).float()
+    V[:, torch.arange(tokens), :, torch.arange(tokens)] = 1.0
+    store = (lambda x: x.to(BF).to(DEV)) if kv == "bf16" else _codes
+    Kp, Vp = (store(x.view(n * columns, page, kv_heads, D)) for x in (K, V))
+    Q = torch.zeros(n, heads, D)
+    Q[:, :, 0] = torch.from_numpy(q0).float()
+    O = torch.empty(n, heads, D, dtype=torch.float32, device=DEV)
+    ws = _workspace(n, heads, kv_heads, D)
+    B.pafu_paged_attention(Q.to(BF).to(DEV), Kp, Vp, ints(np.arange(n * columns).reshape(n, columns)), ints([tokens] * n), O,
+                           softmax_scale=1.0, workspace=ws)
+    assert bool((ws != 0xA5).any()) == (columns > 32)                   # cut or not: as named
+    s = q0[:, :, None] * np.repeat(k0.transpose(0, 2, 1), heads // kv_heads, axis=1)
+    w = np.exp(s - s.max(-1, keepdims=True))
+    w /= w.sum(-1, keepdims=True)
+    got = O.double().cpu().numpy()
+    # In units u = 2^-24.  A score in the exponent of 2 is at most 5.8, the distance to the reference at most 11.6 (and 8 more
+    # where the reference lags).  Scale times log2(e): three roundings, 3 * 11.6 of the distance; the reference's own rounding 5.8,
+    # the distance's 20: 61, times ln 2: 42.  exp2: 2.  That holds for the weight and for the normaliser: 88.  Sums and rescalings of
+    # 64 weights: 24; of a result 8; the division and the product by it: 4.  Weights off by 2^-16 would be off by 256.
+    err = np.abs(got[:, :, :tokens] - w) / w
+    assert err.max() <= 124 * 2.0 ** -24, err.max() * 2.0 ** 24
+    assert bool((O[:, :, tokens:] == 0).all())
+
+
+@pytest.mark.parametrize("columns", [8, 80], ids=["whole", "cut"])
+@pytest.mark.parametrize("heads,kv_heads,D", [(4, 1, 128), (32, 1, 128), (48, 1, 64)])
+def test_attention_infinite_values_under_small_weights(heads, kv_heads, D, columns):
+    # a weight of 2^-x is not 0 as long as fp32 has it: times an infinite value it is infinite
+    page = 16
+    for x in (8, 60, 100, 112, 120, 125):
+        K, V = (torch.zeros(columns, page, 1, D) for _ in range(2))
+        K[:, :, 0, 0] = -1.0
+        K[1, 3, 0, 0] = 0.0                                             # the highest score
+        V[0, 5, 0, 7], V[2, 1, 0, 9], V[1, 3, 0, 2] = math.inf, -math.inf, 1.0
+        Q = torch.zeros(1, heads, D)
+        Q[:, :, 0] = 1.0
+        O = torch.empty(1, heads, D, dtype=torch.float32, device=DEV)
+        B.pafu_paged_attention(Q.to(BF).to(DEV), K.to(BF).to(DEV), V.to(BF).to(DEV), ints(np.arange(columns)[None]), ints([100]), O,
+                               softmax_scale=x * math.log(2.0), workspace=_workspace(1, heads, kv_heads, D))
+        got = O[0].cpu()
+        assert bool((got[:, 7] == math.inf).all() and (got[:, 9] == -math.inf).all()), x
+        rest = [d for d in range(D) if d not in (7, 9)]
+        assert bool(torch.isfinite(got[:, rest]).all()), x
