@@ -211,7 +211,7 @@ __global__ __launch_bounds__(kTableThreads) void paged_tables_kernel(PagedTables
       store4(t.kv_len_out, b0, t.B, total);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (b0 + e < t.B && first[b0 + e + 1] > at[e] && pages_of(s[e]) < t.max_pages)
+        if (b0 + e < t.B && pages_of(total[e]) > pages_of(s[e]) && pages_of(s[e]) < t.max_pages)
           t.table[(b0 + e) * t.ld_table + pages_of(s[e])] = page[e];
     }
   }
@@ -225,12 +225,18 @@ __global__ __launch_bounds__(kTableThreads) void paged_tables_kernel(PagedTables
     // through 64 of its (request, run) pairs at once for those that are not empty
     const int waves = gridDim.x * kTableWaves, id = blockIdx.x * kTableWaves + wave, parts = max(waves / t.B, 1);
     const int jobs = t.B * parts;
+    // what a request takes: a difference of the sums, unless they are saturated
+    auto pages_taken = [&](int b) {
+      const int end = first[b + 1];
+      if (end < 0x7fffffff) return end - first[b];
+      return pages_of(sat_add(begin[b], max(t.count[b], 0))) - pages_of(begin[b]);
+    };
     for (int j0 = id; j0 < jobs; j0 += waves * 64) {
       const int j = j0 + lane * waves, mine = j < jobs ? j % t.B : 0;
-      for (unsigned long long todo = __ballot(j < jobs && first[mine + 1] - first[mine] > 1 + j / t.B * 64); todo;
+      for (unsigned long long todo = __ballot(j < jobs && pages_taken(mine) > 1 + j / t.B * 64); todo;
            todo &= todo - 1) {
         const int job = j0 + (__ffsll(todo) - 1) * waves, b = job % t.B, part = job / t.B, from = first[b];
-        const int have = pages_of(begin[b]), in_table = min(first[b + 1] - from, t.max_pages - have);
+        const int have = pages_of(begin[b]), in_table = min(pages_taken(b), t.max_pages - have);
         for (int i = 1 + part * 64 + lane; i < in_table; i += parts * 64) {
           const int at = sat_add(from, i);
           t.table[b * t.ld_table + have + i] = at < t.n_free ? t.free_pages[at] : -1;

@@ -1,4 +1,5 @@
-"""Attention of one new token at the limits of its numbers: the bits of its weights, infinities, rows that see nothing."""
+"""The paged K/V cache at the limits of its numbers: sums of pages that saturate, the bits of the attention's weights, infinities,
+rows that see nothing."""
 import math
 
 import numpy as np
@@ -8,6 +9,7 @@ import torch
 from oracle import pafu_oracle as orc
 from paper_2601_21896_amd import binding as B
 from tests.gpu_util import DEV
+from tests.test_gpu_paged import _tables
 
 pytestmark = pytest.mark.gpu
 BF = torch.bfloat16
@@ -82,3 +84,14 @@ def test_attention_infinite_values_under_small_weights(heads, kv_heads, D, colum
         assert bool((got[:, 7] == math.inf).all() and (got[:, 9] == -math.inf).all()), x
         rest = [d for d in range(D) if d not in (7, 9)]
         assert bool(torch.isfinite(got[:, rest]).all()), x
+
+
+@pytest.mark.parametrize("kv,new,page,start", [
+    ([0, 0], [8, 8], 8, 2 ** 31 - 2),
+    ([3, 5, 0, 100, 7], [40, 600, 0, 30, 1], 8, 2 ** 31 - 3),
+    ([0, 0, 3], [5000, 2500, 900], 16, 2 ** 31 - 200),
+    ([16] * 300, [33] * 300, 16, 2 ** 31 - 100),
+    ([0, 9], [20, 20], 8, 2 ** 31 - 1)],
+                         ids=["one page each", "within a request", "many pages", "300 requests", "from the start"])
+def test_tables_enter_pages_behind_a_saturated_sum_as_missing(kv, new, page, start):
+    _tables(kv, new, 5, page, max(-(-(a + b) // page) for a, b in zip(kv, new)), sum(new) + 3, start, extra_ld=1)
