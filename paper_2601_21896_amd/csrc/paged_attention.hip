@@ -137,6 +137,12 @@ __device__ __forceinline__ u16x2 upper_halves(float x, float y) {
   return __builtin_bit_cast(u16x2, __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u));
 }
 
+// x y; 0 where y is 0, whatever x: a row whose scores are all -infinity is 0 even if 0 times its values gave NaN
+__device__ __forceinline__ f32x4 scaled(f32x4 x, float y) {
+  const unsigned keep = y == 0.f ? 0u : ~0u;
+  return __builtin_bit_cast(f32x4, __builtin_bit_cast(u32x4, x * y) & keep);
+}
+
 // two codes of a word -> two bf16 (exact; the tensor's scale is applied elsewhere)
 __device__ __forceinline__ unsigned widen2(unsigned w, bool upper) {
   return upper ? __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true))
@@ -518,7 +524,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
                 y[k] = f32x4{o[qt][4 * k][r], o[qt][4 * k + 1][r], o[qt][4 * k + 2][r], o[qt][4 * k + 3][r]};
             }
 #pragma unroll
-            for (int k = 0; k < kBlocks / 4; ++k) y[k] *= inv;
+            for (int k = 0; k < kBlocks / 4; ++k) y[k] = scaled(y[k], inv);
             if (!whole || out_bytes == 4) {
               char* to = whole ? static_cast<char*>(a.O) + p0.b * a.ld_o + (h * D + elements) * 4
                                : reinterpret_cast<char*>(ly.partial + (slot * a.N + h) * D + elements);
@@ -637,7 +643,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttention a, Layou
     l += sl[i] * w;
     o += so[i][lane] * w;
   }
-  o *= l == 0.f ? 0.f : a.v_scale / l;
+  o = scaled(o, l == 0.f ? 0.f : a.v_scale / l);
   char* to = static_cast<char*>(a.O) + b * a.ld_o + ((long long)h * D + first + lane * 4) * (OUT_F32 ? 4 : 2);
   if constexpr (OUT_F32) {
     *reinterpret_cast<f32x4*>(to) = o;

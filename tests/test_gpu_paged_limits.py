@@ -95,3 +95,18 @@ def test_attention_infinite_values_under_small_weights(heads, kv_heads, D, colum
                          ids=["one page each", "within a request", "many pages", "300 requests", "from the start"])
 def test_tables_enter_pages_behind_a_saturated_sum_as_missing(kv, new, page, start):
     _tables(kv, new, 5, page, max(-(-(a + b) // page) for a, b in zip(kv, new)), sum(new) + 3, start, extra_ld=1)
+
+
+@pytest.mark.parametrize("columns", [8, 80], ids=["whole", "cut"])
+@pytest.mark.parametrize("heads,kv_heads,D", [(4, 1, 128), (8, 8, 64), (48, 1, 64)])
+def test_attention_of_scores_that_are_all_minus_infinity_is_0_whatever_the_values(heads, kv_heads, D, columns):
+    page = 16
+    K, V = (torch.ones(2 * columns, page, kv_heads, D, dtype=BF, device=DEV) for _ in range(2))
+    K[:columns] = -math.inf
+    V[0, 0], V[0, 1], V[1, 1] = math.inf, math.nan, -math.inf
+    for tokens in (1, 20, 100):
+        O = torch.full((2, heads, D), 9.0, dtype=torch.float32, device=DEV)
+        B.pafu_paged_attention(torch.ones(2, heads, D, dtype=BF, device=DEV), K, V, ints(np.arange(2 * columns).reshape(2, columns)),
+                               ints([tokens, tokens]), O, workspace=_workspace(2, heads, kv_heads, D))
+        assert bool((O[0] == 0).all()), tokens
+        assert bool((O[1] == 1).all()), tokens
