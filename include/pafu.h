@@ -286,7 +286,8 @@ int pafu_paged_append(void* stream, const void* K, const void* V, long long ld_i
  * value it is NaN.
  * Results do not depend on timing; where requests are cut depends on the lengths in the call, which moves the last
  * bits of an fp32 result.  Calls that may overlap in time need workspaces of their own.  PAFU_ERR_SHAPE where
- * the table's room, B * ceil(max_pages * page_size / 32), passes 2^31 - 1, or B * N does 2^24 - 1.
+ * the table's room, B * ceil(max_pages * page_size / 32), with B added for a window behind pinned tokens, passes 2^31 - 1, or
+ * B * N does 2^24 - 1.
  */
 size_t pafu_paged_attention_workspace_bytes(int B, int N, int N_kv, int D);
 int pafu_paged_attention(void* stream, const void* Q, long long ld_q, const void* K_pages, const void* V_pages,

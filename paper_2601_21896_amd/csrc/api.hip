@@ -932,7 +932,8 @@ int pafu_paged_attention(void* stream, const void* Q, long long ld_q, const void
   if (rc) return rc;
   if (N < 1 || N > (1 << 16) - 1 || N % N_kv != 0 || n_pinned < 0 || window < 0) return PAFU_ERR_SHAPE;
   const long long row_tokens = (long long)max_pages << pool.page_log2, max_tokens = row_tokens < 0x7fffffff ? row_tokens : 0x7fffffff;
-  if (B > 0 && (max_tokens + 31) / 32 > 0x7fffffffll / B) return PAFU_ERR_SHAPE;  // the tiles of all requests: 32 bits
+  // the tiles of all requests: 32 bits.  Behind a sink a window may begin inside a tile: a request has one more then.
+  if (B > 0 && (max_tokens + 31) / 32 + (window > 0 && n_pinned > 0) > 0x7fffffffll / B) return PAFU_ERR_SHAPE;
   if ((long long)B * N >= (1 << 24)) return PAFU_ERR_SHAPE;  // a launch's threads: 32 bits
   const int ob = dtype_bytes(out_dtype);
   if (ob == 0) return PAFU_ERR_DTYPE;

@@ -1,0 +1,35 @@
+"""The paged calls at the limits of what they accept, on the host (no GPU needed).  Calls that are to be accepted pass NULL for
+Q, which is told after the shapes: nothing is launched."""
+from paper_2601_21896_amd import binding as B
+
+A = 0x10000  # a fake, 16-byte aligned "device address"
+MB = 0x100000
+
+
+def _attention(**kw):
+    a = dict(Q=None, ldq=1024, Kp=A + 0x10000000, Vp=A + 0x20000000, np=10, ps=32, ldp=32 * 256, ldt=256, ldh=128, dt=0, ks=0, vs=0,
+             table=A + MB, mp=8, ld=8, kv=A + 2 * MB, B=4, N=8, Nkv=2, D=128, pin=0, win=0, sc=0.0, O=A + 3 * MB, ldo=1024, od=0,
+             ws=None, wsb=0)
+    a.update(kw)
+    return B.library().pafu_paged_attention(None, *a.values())
+
+
+def _tiles(length, window, pinned):
+    """32-token tiles that hold a request's visible tokens, those of the sink and those of the window in tiles of their own."""
+    lo = length - window if 0 < window < length else 0
+    pin = min(pinned, length) if lo > min(pinned, length) else 0
+    lo = lo if pin or lo > pinned else 0
+    return -(-pin // 32) + (-(-(length - lo // 32 * 32) // 32))
+
+
+def test_attention_refuses_more_tiles_than_32_bits_count_with_a_sink_too():
+    columns = (2 ** 31 - 1) // 8192                     # of 32 tokens: a tile each
+    assert 8192 * columns < 2 ** 31 <= 8192 * (columns + 1)
+    # a sink and a window that begins inside a tile: one tile more than the table has room for
+    assert _tiles(columns * 32, columns * 32 - 17, 1) == columns + 1
+    assert _tiles(columns * 32, columns * 32 - 17, 0) == _tiles(columns * 32, 0, 1) == columns
+    big = dict(B=8192, mp=columns, ld=columns)
+    assert _attention(**big) == _attention(**big, win=columns * 32 - 17) == _attention(**big, pin=1) == -1
+    assert _attention(**big, win=columns * 32 - 17, pin=1) == -2
+    assert _attention(**dict(big, mp=columns - 1), win=columns * 32 - 17, pin=1) == -1
+    assert _attention(**dict(big, mp=columns + 1, ld=columns + 1)) == -2
