@@ -177,14 +177,17 @@ int check_pool(const void* K, const void* V, int n_pages, int page_size, long lo
                    n_pages, log2};
   return PAFU_OK;
 }
-// What a pool's tensor spans: tokens at one stride where the pages follow each other without a gap (K and V may then lie
-// side by side in a token), pages otherwise.
-Span pool_span(const void* p, const PagedPool& pool, int N, int D, int dtype) {
-  const long long page_size = 1ll << pool.page_log2;
-  const long long token = (N - 1) * pool.ld_head + (long long)D * kv_dtype_bytes(dtype);
-  if (pool.ld_page == page_size * pool.ld_token && pool.ld_token >= token)
-    return Span{p, pool.n_pages * page_size, pool.ld_token, token};
-  return Span{p, pool.n_pages, pool.ld_page, (page_size - 1) * pool.ld_token + token};
+// What a pool's tensor spans, as rows of one kind at one stride: pages, tokens, or a head's tokens (the latter two where the
+// pages are a multiple of them apart, or there is one page, whose stride says nothing).  Each covers all that the pool holds, and
+// K and V may lie side by side in any of the three ways: where they are apart in one kind they are apart.
+enum PoolRows { kPages, kTokens, kHeads, kPoolRows };
+Span pool_span(const void* p, const PagedPool& pool, int N, int D, int dtype, int kind) {
+  const long long page_size = 1ll << pool.page_log2, element = (long long)D * kv_dtype_bytes(dtype);
+  const long long token = (N - 1) * pool.ld_head + element, head = (page_size - 1) * pool.ld_token + element;
+  const long long row = kind == kTokens ? token : head, ld = kind == kTokens ? pool.ld_token : pool.ld_head;
+  if (kind == kPages || ld < row || (pool.n_pages > 1 && pool.ld_page % ld != 0))
+    return Span{p, pool.n_pages, pool.ld_page, (page_size - 1) * pool.ld_token + token};
+  return Span{p, (kind == kTokens ? page_size : N) + (pool.n_pages - 1) * (pool.ld_page / ld), ld, row};
 }
 // Does any of `outs` overlap another of them or any of `ins`?
 template <int N_OUT, int N_IN>
@@ -907,8 +910,12 @@ int pafu_paged_append(void* stream, const void* K, const void* V, long long ld_i
   if (!K || !V || !slots) return PAFU_ERR_NULL;
   if (!aligned16(K) || !aligned16(V) || !aligned16(slots) || (ld_in * 2) % 16 != 0) return PAFU_ERR_ALIGN;
   const Span ins[] = {{K, rows, ld_in * 2, row * 2}, {V, rows, ld_in * 2, row * 2}, {slots, 1, 0, rows * 4ll}};
-  const Span outs[] = {pool_span(K_pages, pool, N, D, kv_dtype), pool_span(V_pages, pool, N, D, kv_dtype)};
-  if (any_overlap(outs, ins)) return PAFU_ERR_ALIAS;
+  bool apart = false;
+  for (int kind = kPages; kind < kPoolRows && !apart; ++kind) {
+    const Span outs[] = {pool_span(K_pages, pool, N, D, kv_dtype, kind), pool_span(V_pages, pool, N, D, kv_dtype, kind)};
+    apart = !any_overlap(outs, ins);
+  }
+  if (!apart) return PAFU_ERR_ALIAS;
   return launch_paged_append(static_cast<hipStream_t>(stream), K, V, ld_in * 2, rows, slots, N, D, pool, kv_dtype,
                              k_scale_log2, v_scale_log2);
 }
@@ -946,11 +953,15 @@ int pafu_paged_attention(void* stream, const void* Q, long long ld_q, const void
       (ld_o * ob) % 16 != 0)
     return PAFU_ERR_ALIGN;
   if (workspace != nullptr && workspace_bytes > 0 && !aligned16(workspace)) return PAFU_ERR_ALIGN;
-  const Span ins[] = {{Q, B, ld_q * 2, row * 2}, pool_span(K_pages, pool, N_kv, D, kv_dtype),
-                      pool_span(V_pages, pool, N_kv, D, kv_dtype), {block_table, B, ld_table * 4, max_pages * 4ll},
-                      {kv_len, 1, 0, B * 4ll}};
   const Span outs[] = {{O, B, ld_o * ob, row * ob}, {workspace, 1, 0, (long long)workspace_bytes}};
-  if (any_overlap(outs, ins)) return PAFU_ERR_ALIAS;
+  bool apart = false;
+  for (int kind = kPages; kind < kPoolRows && !apart; ++kind) {
+    const Span ins[] = {{Q, B, ld_q * 2, row * 2}, pool_span(K_pages, pool, N_kv, D, kv_dtype, kind),
+                        pool_span(V_pages, pool, N_kv, D, kv_dtype, kind), {block_table, B, ld_table * 4, max_pages * 4ll},
+                        {kv_len, 1, 0, B * 4ll}};
+    apart = !any_overlap(outs, ins);
+  }
+  if (!apart) return PAFU_ERR_ALIAS;
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)D);
   const bool kv8 = kv_dtype == PAFU_FP8_E4M3;
   const PagedAttention a{Q, O, block_table, kv_len, ld_q * 2, ld_o * ob, ld_table, B, N, N_kv, D, max_pages, (int)max_tokens,

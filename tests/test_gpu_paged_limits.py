@@ -6,10 +6,11 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import paged_oracle as po
 from oracle import pafu_oracle as orc
 from paper_2601_21896_amd import binding as B
 from tests.gpu_util import DEV
-from tests.test_gpu_paged import _tables
+from tests.test_gpu_paged import _tables, bf16_values
 
 pytestmark = pytest.mark.gpu
 BF = torch.bfloat16
@@ -110,3 +111,37 @@ def test_attention_of_scores_that_are_all_minus_infinity_is_0_whatever_the_value
                                ints([tokens, tokens]), O, workspace=_workspace(2, heads, kv_heads, D))
         assert bool((O[0] == 0).all()), tokens
         assert bool((O[1] == 1).all()), tokens
+
+
+def _side_by_side(layout, n_pages, page, heads, D, dtype):
+    """A slab of numbers, and how K and V lie in it."""
+    shape, views = {
+        "rows alternate": ((n_pages, page, 2, heads, D), lambda s: (s[:, :, 0], s[:, :, 1])),
+        "rows alternate, gaps": ((n_pages, page + 3, 2, heads + 1, D), lambda s: (s[:, :page, 1, :heads], s[:, 1:page + 1, 0, 1:])),
+        "heads alternate": ((n_pages, heads, 2, page, D), lambda s: (s[:, :, 1].permute(0, 2, 1, 3), s[:, :, 0].permute(0, 2, 1, 3))),
+        "pages alternate": ((n_pages, 2, page, heads, D), lambda s: (s[:, 1], s[:, 0])),
+        "pages and heads alternate": ((n_pages, 2, heads, page, D), lambda s: (s[:, 0].permute(0, 2, 1, 3), s[:, 1].permute(0, 2, 1, 3))),
+    }[layout]
+    count = int(np.prod(shape))
+    numbers = torch.arange(count, dtype=torch.int32) * 7919 % 251
+    return (numbers.to(BF) if dtype == BF else numbers.to(torch.uint8)).view(shape), views
+
+
+@pytest.mark.parametrize("n_pages", [1, 3])
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads,D", [(1, 64), (3, 128)])
+@pytest.mark.parametrize("layout", ["rows alternate", "rows alternate, gaps", "heads alternate", "pages alternate",
+                                    "pages and heads alternate"])
+def test_append_to_pools_that_lie_side_by_side(layout, heads, D, kv, n_pages):
+    page, dtype = 16, BF if kv == "bf16" else torch.uint8
+    rng = np.random.default_rng(heads + n_pages)
+    slab, views = _side_by_side(layout, n_pages, page, heads, D, dtype)
+    slots = rng.permutation(n_pages * page)[:13]
+    rows = [bf16_values(rng, 13, heads, D) for _ in range(2)]
+    on_gpu = slab.to(DEV)
+    B.pafu_paged_append(*(x.to(DEV) for x in rows), ints(slots), *views(on_gpu))
+    want = slab.clone().view(torch.int16 if dtype == BF else torch.uint8)
+    for t, x in zip(views(want), rows):
+        new = x.view(torch.int16).numpy() if dtype == BF else orc.quantise_e4m3(x.double().numpy(), 0)
+        t.copy_(torch.from_numpy(po.paged_append(t.numpy(), new, slots)))
+    assert torch.equal(on_gpu.cpu().view(want.dtype), want)

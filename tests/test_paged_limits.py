@@ -33,3 +33,24 @@ def test_attention_refuses_more_tiles_than_32_bits_count_with_a_sink_too():
     assert _attention(**big, win=columns * 32 - 17, pin=1) == -2
     assert _attention(**dict(big, mp=columns - 1), win=columns * 32 - 17, pin=1) == -1
     assert _attention(**dict(big, mp=columns + 1, ld=columns + 1)) == -2
+
+
+def _append(**kw):
+    a = dict(K=A, V=A + MB, ld=256, rows=20, slots=A + 2 * MB, N=2, D=128, Kp=A + 0x10000000, Vp=A + 0x20000000, np=10, ps=16,
+             ldp=16 * 256, ldt=256, ldh=128, dt=0, ks=0, vs=0)
+    a.update(kw)
+    return B.library().pafu_paged_append(None, *a.values())
+
+
+def test_append_refuses_pools_that_share_a_byte_on_one_page_too():
+    K = A + 0x10000000
+    for pages in (1, 2, 10):
+        # rows of 256 elements at a stride of 512, V's shifted: by less than a row, by so much that they reach the next of K's
+        for shift in (0, 8, 248, 264, 504, 512, 512 * 3 + 248):
+            for sign in (1, -1):
+                assert _append(Vp=K + sign * shift * 2, np=pages, ldt=512, ldp=16 * 512) == -6, (pages, shift, sign)
+                assert _append(Vp=K + sign * shift * 2, np=pages, ldt=512, ldp=17 * 512) == -6, (pages, shift, sign)
+        # tokens inside heads: 16 * 128 elements at a stride of 4096
+        for shift in (0, 8, 2040, 2056, 4088, 4096):
+            assert _append(Vp=K + shift * 2, np=pages, ldt=128, ldh=4096, ldp=2 * 4096) == -6, (pages, shift)
+    assert _append(Kp=A - 0x1000, Vp=K, np=1) == _append(Kp=K, Vp=A + 2 * MB - 64, np=1) == -6    # over rows, over slots
