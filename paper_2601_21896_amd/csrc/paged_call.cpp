@@ -111,14 +111,17 @@ struct Call {
   }
 };
 
-// A page pool: both tensors [n_pages, page_size, N_kv, D], of one type, shape and stride, elements contiguous.
+// A page pool: both tensors [n_pages, page_size, N_kv, D], of one type, shape and stride (that of an axis of length one is not
+// read), elements contiguous.
 struct Pool {
   void *K, *V;
   int n_pages, page_size, N, D, dtype;
   long long ld_page, ld_token, ld_head;
   Pool(Call& call, PyObject* k_obj, PyObject* v_obj) {
     const at::Tensor &k = call.tensor(k_obj, "K_pages"), &v = call.tensor(v_obj, "V_pages");
-    if (k.dim() != 4 || v.sizes() != k.sizes() || v.strides() != k.strides() || k.stride(3) != 1)
+    bool alike = k.dim() == 4 && v.sizes() == k.sizes();
+    for (int i = 0; alike && i < 4; ++i) alike = k.size(i) == 1 || v.stride(i) == k.stride(i);
+    if (!alike || k.stride(3) != 1)
       refuse(PyExc_ValueError, "the page tensors must be [n_pages, page_size, N_kv, D] of one shape and stride, elements contiguous");
     if (v.scalar_type() != k.scalar_type() || (k.scalar_type() != at::kBFloat16 && k.scalar_type() != at::kByte))
       refuse(PyExc_TypeError, "page tensors are bfloat16 or uint8 (E4M3 codes), not %s and %s", c10::toString(k.scalar_type()),

@@ -1,5 +1,8 @@
 """The paged calls at the limits of what they accept, on the host (no GPU needed).  Calls that are to be accepted pass NULL for
 Q, which is told after the shapes: nothing is launched."""
+import pytest
+import torch
+
 from paper_2601_21896_amd import binding as B
 
 A = 0x10000  # a fake, 16-byte aligned "device address"
@@ -54,3 +57,22 @@ def test_append_refuses_pools_that_share_a_byte_on_one_page_too():
         for shift in (0, 8, 2040, 2056, 4088, 4096):
             assert _append(Vp=K + shift * 2, np=pages, ldt=128, ldh=4096, ldp=2 * 4096) == -6, (pages, shift)
     assert _append(Kp=A - 0x1000, Vp=K, np=1) == _append(Kp=K, Vp=A + 2 * MB - 64, np=1) == -6    # over rows, over slots
+
+
+def test_binding_does_not_read_the_strides_of_axes_of_length_one():
+    # one head or one page: K by tokens, V by heads is the same memory.  On the host such a pool gets as far as the check of its place.
+    i, table = torch.zeros(4, dtype=torch.int32), torch.zeros(4, 1, dtype=torch.int32)
+    one_head = torch.zeros(3, 16, 1, 64, dtype=torch.bfloat16), torch.zeros(3, 1, 16, 64, dtype=torch.bfloat16).permute(0, 2, 1, 3)
+    wide = torch.zeros(2, 40, 2, 64, dtype=torch.bfloat16)
+    one_page = torch.zeros(1, 16, 2, 64, dtype=torch.bfloat16), wide[1:, :16]
+    for K, V in (one_head, one_page):
+        assert K.shape == V.shape and K.stride() != V.stride()
+        rows = torch.zeros(4, K.shape[2], 64, dtype=torch.bfloat16)
+        for pages in ((K, V), (V, K)):
+            with pytest.raises(ValueError, match="GPU"):
+                B.pafu_paged_append(rows, rows, i, *pages)
+            with pytest.raises(ValueError, match="GPU"):
+                B.pafu_paged_attention(rows, *pages, table, i, rows)
+    K, V = torch.zeros(3, 16, 2, 64, dtype=torch.bfloat16), torch.zeros(3, 2, 16, 64, dtype=torch.bfloat16).permute(0, 2, 1, 3)
+    with pytest.raises(ValueError, match="one shape and stride"):
+        B.pafu_paged_append(torch.zeros(4, 2, 64, dtype=torch.bfloat16), torch.zeros(4, 2, 64, dtype=torch.bfloat16), i, K, V)
