@@ -45,6 +45,8 @@ def build_call() -> str:
     """Compiles the Python module that hands torch tensors to the paged calls (no GPU code)."""
     import sysconfig
 
+    if os.path.exists(CALL):  # one that does not belong to the library is worse than none
+        os.remove(CALL)
     import torch
     torch_dir = os.path.dirname(torch.__file__)
     include, lib_dir = os.path.join(torch_dir, "include"), os.path.join(torch_dir, "lib")
@@ -73,9 +75,9 @@ def build(verbose: bool = False, extra_flags=(), out: str = "") -> str:
     with ThreadPoolExecutor(max_workers=min(len(SOURCES), 8)) as ex:
         call = ex.submit(build_call) if not out else None
         logs = list(ex.map(one, range(len(SOURCES))))
-        if call is not None:
-            logs.append(call.result())
     logs.append(_run([cc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]))
+    if call is not None:  # (the library is there whether or not torch's headers fit the module)
+        logs.append(call.result())
     if verbose:
         print("\n".join(l for l in logs if l.strip()))
     return LIB
