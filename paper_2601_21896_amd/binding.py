@@ -169,11 +169,17 @@ def _ptr(t):
     return t.data_ptr()
 
 
+def _raw_stream():
+    """device index -> the current stream's handle.  Torch's short way, which builds no Stream object around it (0.5 us instead
+    of 2.7), is not part of its public interface: without it, the public one."""
+    import torch
+    return getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _stream(stream):
     if stream is None:
         import torch
-        # the current stream's handle without building the Stream object around it (0.3 us instead of 2.7)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return _raw_stream()(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -460,7 +466,7 @@ def _paged():
                                % (call.torch_version, torch.__version__))
         call.bind(*(ctypes.cast(f, c_void_p).value for f in (lib.pafu_paged_tables, lib.pafu_paged_slots,
                                                              lib.pafu_paged_append, lib.pafu_paged_attention)),
-                  torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+                  getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device, _raw_stream())
         _PAGED = lib, call
     return _PAGED[1]
 
