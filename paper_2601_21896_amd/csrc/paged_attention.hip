@@ -725,16 +725,19 @@ size_t paged_attention_workspace_bytes(int B, int N, int N_kv, int D) {
 int launch_paged_attention(hipStream_t st, const PagedAttention& a, const PagedPool& pool, void* workspace,
                            size_t workspace_bytes) {
   Layout ly;
-  ly.groups = query_groups(a.N, a.N_kv, a.D).groups;
+  const Groups split = query_groups(a.N, a.N_kv, a.D);
+  ly.groups = split.groups;
   ly.heads = a.N_kv * ly.groups;
   const long long longest = ((long long)a.max_tokens + kTile - 1) / kTile, items = (long long)a.B * ly.heads;
   const int units = compute_units();
   // Short requests are not cut: the join and the way to it (7 us) cost more than an even share is worth.  By the most tiles that
   // a request may have, cut -> whole: 8 tiles, 100 requests of 150 .. 250 tokens, 32 / 8 heads of 128, 26.5 -> 18.9 us; 16
   // tiles, 256 of 300 .. 512 86 -> 73 us, 400 of 100 .. 500 with one key head 27 -> 18; 32 tiles, 4 of 300 .. 1000 11.5 -> 17.4.
-  // With more than 512 waves (two workgroups to a unit) and less than 2048 (all that fit) the longest ones decide: 16 tiles, 128
-  // of 100 .. 512 with 12 / 12 heads 40 -> 51.
-  const bool one_round = ly.heads >= kWaves && items > 2 * units && items < 8 * units;
+  // With more than 512 waves (two workgroups to a unit) and less than 2048 (all that fit) the longest ones decide, and how much
+  // longer than the others they are the host does not know.  At 512 to 2048 waves, 9 .. 16 tiles, cut / whole on the average of 25
+  // shapes: 1 .. 400 tokens 0.84 (0.66 .. 1.00), 100 .. 512 0.99, 300 .. 512 1.10, 500 .. 512 1.14 (1.00 .. 1.27): cut, for batches
+  // are ragged.  Not with more than 16 query heads to a key head, whose partial results are as many: 1.41 (0.92 .. 1.80) of 47.
+  const bool one_round = split.groups * split.qt == 1 && ly.heads >= kWaves && items > 2 * units && items < 8 * units;
   ly.cut = workspace != nullptr && workspace_bytes >= paged_attention_workspace_bytes(a.B, a.N, a.N_kv, a.D) &&
            longest > (one_round ? 8 : 16);
   ly.columns = a.B;

@@ -68,6 +68,15 @@ def test_attention_of_many_short_requests(cut, heads, kv_heads, D, kv):
     assert not any(cut)
 
 
+@pytest.mark.parametrize("heads,kv_heads,D,cuts", [(16, 4, 128, True), (64, 4, 64, True), (68, 4, 128, False), (96, 4, 64, False),
+                                                   (128, 4, 64, False)])
+def test_attention_of_up_to_512_tokens_is_cut_for_few_query_heads_to_a_key_head(cut, heads, kv_heads, D, cuts):
+    # 560 waves and more: two workgroups to a unit, not four
+    rng = np.random.default_rng(heads)
+    t._attend(list(rng.integers(1, 401, 140)), heads, kv_heads, D, 16, out=torch.float32, columns=25)
+    assert cut == [cuts]
+
+
 @pytest.mark.parametrize("n,kv", [(63, "bf16"), (64, "e4m3"), (65, "bf16"), (130, "e4m3"), (300, "bf16"), (700, "bf16")])
 @pytest.mark.parametrize("window,pinned", [(0, 0), (100, 20), (31, 700), (600, 1)])
 def test_attention_of_cut_batches_with_windows(cut, n, kv, window, pinned):
