@@ -225,7 +225,8 @@ int pafu_chunk_attention_fp8(void* stream, const void* Q, int Lq, const void* Kc
  * not read.
  * Request b's tokens lie in order on the pages block_table[b * ld_table + 0, 1, ...]; the slot of a token is
  * page * page_size + its place on the page.  In a pool with heads inside tokens and no gaps slots are row numbers of the
- * pool seen as [n_pages * page_size, N_kv, D]: pafu_chunk_attention_gather and pafu_compact_kv take them as ids.
+ * pool seen as [n_pages * page_size, N_kv, D]: pafu_compact_kv takes them as ids, and so does pafu_chunk_attention_gather for
+ * a bf16 pool of less than 4 GiB a tensor, as many query heads as key heads, and a list without -1.
  * All lengths, tables and slots are int32 on the device and are read when the kernels run, so that a captured graph
  * follows them; nothing in them can make a kernel leave its buffers (what is out of range takes no part, as said below).
  * Shapes are what the launch is sized for: requests of a padded batch have length 0.  At most

@@ -338,7 +338,9 @@ int launch_paged_append(hipStream_t st, const void* K, const void* V, long long 
   a.step_r = (unsigned)(blocks * 256 / a.chunks);
   a.step_c = (unsigned)(blocks * 256 % a.chunks);
   const bool codes = kv_dtype == PAFU_FP8_E4M3;
-  // past the caches from 64 MiB of rows on (measured better from 128 MiB, worse up to 32)
+  // Past the caches from 64 MiB of rows on.  Through -> past them, with six sets of rows and pages in turn, which the caches do
+  // not hold: 16 MiB 7.8 -> 8.1 us, 32 17.2 -> 14.1, 64 28.8 -> 25.8, 128 53.1 -> 50.4; with two, which they hold in part: 32 14.8
+  // -> 15.0, 48 19.1 -> 20.7, 64 25.8 -> 26.5, 80 34.7 -> 32.8, 128 54.2 -> 51.2 (codes and other layouts alike).
   const bool stream = (long long)rows * N * D * 4 >= 64ll << 20;
   const auto kernel = codes ? (stream ? paged_append_kernel<true, true> : paged_append_kernel<true, false>)
                             : (stream ? paged_append_kernel<false, true> : paged_append_kernel<false, false>);

@@ -11,10 +11,10 @@
 // by byte permutes; column n of block i is element 8 n + i.  O^T has the queries in columns like S^T, so that a raise of
 // the softmax reference is a multiplication in the lane.
 //
-// Bound by the reads of K and V, at up to 6.85 TB/s (a kernel that only reads reaches 7.0; a large copy 5.2).  They bypass the
-// caches where one wave alone reads their lines (6.2 TB/s otherwise), except in small calls.  Eight waves per compute unit, all of the launch at once, hold
-// enough rows in flight; twelve or sixteen were slower everywhere (more, shorter runs).  What a call takes beyond the reads:
-// about 5 us until the first rows are there, 7 us for the join and the way to it.
+// Bound by the reads of K and V, at up to 6.9 TB/s (a kernel that only reads reaches 7.0; a large copy 5.1).  They bypass the
+// caches where one wave alone reads their lines (6.2 TB/s otherwise), except in small calls.  Eight waves per compute unit,
+// all of the launch at once, hold enough rows in flight; twelve or sixteen were slower everywhere (more, shorter runs).
+// What a call takes beyond the reads: about 5 us until the first rows are there, 7 us for the join and the way to it.
 //
 // Products of bf16 or widened 8-bit values are exact in fp32.  A weight goes into the second product whole: as the sum of
 // three bf16 numbers, which hold eight of its 24 bits each.
@@ -746,7 +746,7 @@ int launch_paged_attention(hipStream_t st, const PagedAttention& a, const PagedP
   ly.stat = nullptr;
   ly.joins = nullptr;
   // Cut: wide where a workgroup's four heads would not be neighbours in memory; narrow where waves share what they read, so that
-  // they do so through one compute unit's cache (48 / 1 heads of 128 202 -> 154 us; 8-bit rows of 64, 8 / 2 heads, 112 -> 72).
+  // they do so through one compute unit's cache (48 / 1 heads of 128 202 -> 156 us; 8-bit rows of 64, 8 / 2 heads, 112 -> 72).
   // Whole: wide where the requests may be long, or where the launch has few waves.
   const bool wide = ly.cut ? ly.groups == 1 && ((ly.heads < kWaves && !shared_lines(a, pool)) || pool.ld_head > pool.ld_token)
                            : longest > 16 || items <= 2 * units;
