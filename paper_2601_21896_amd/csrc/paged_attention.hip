@@ -1,7 +1,7 @@
 // Attention of one new token per request over a paged K/V cache.
 // (Beyond the paper, whose queries come a chunk at a time.)
 //
-//   O[b,h] = sum_j w_j v[j] / sum_j w_j,   w_j = 2^(s_j - m),   s_j = scale * log2(e) * q[b,h] . k[j]
+//   O[b,h] = sum_j w_j v[j] / sum_j w_j,   w_j = 2^(c (s_j - m)),   s_j = q[b,h] . k[j],   c = scale * log2(e)
 //
 // The tokens of a request are taken in tiles of 32, a wave works on a tile alone.  It forms S^T = K Q^T (16 query heads that
 // share a key head as columns), the weights, and O^T += V^T W^T, all on 16x16x32 matrix instructions.  The rows of the two
@@ -32,8 +32,8 @@ typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kNoMax = -3.0e38f;   // softmax reference before the first visible token
-constexpr float kRaiseAt = 8.f;      // weights up to 2^8: the reference is raised when a score passes it by more
+constexpr float kNoMax = -3.4028235e38f;  // softmax reference m before the first visible token
+constexpr float kRaiseAt = 8.f;           // weights up to 2^8: the reference is raised when a score passes it by more
 constexpr int kTile = 32;            // tokens
 constexpr int kWaves = 4;            // per workgroup
 
@@ -73,6 +73,11 @@ __device__ __forceinline__ Tiles request_tiles(const PagedAttention& a, int kv_l
   t.base = t.lo & ~(kTile - 1);
   t.n = t.n_pin + (t.lo < t.len ? tiles_of(t.len - t.base) : 0);
   return t;
+}
+
+// c.  Not 0: what is not visible is -infinity times it.
+__device__ __forceinline__ float exponent_scale(const PagedAttention& a) {
+  return fmaxf(a.scale * a.k_scale * kLog2e, 1.1754944e-38f);
 }
 
 // inclusive sums over the wave's lanes
@@ -225,7 +230,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
 
   // joins are told by request, or by column with the request in the first place
   const bool by_request = ly.cut && ly.joined == a.B, tells = ly.cut && head_id == 0 && sub == 0 && lane == 0;
-  const float sc = fmaxf(a.scale * a.k_scale * kLog2e, 1.1754944e-38f);  // not 0: what is not visible is -infinity times it
+  const float sc = exponent_scale(a);
   int2 join = make_int2(0, 0);  // of the column
   if (!ly.cut) {
     kv0 = b;
@@ -413,21 +418,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
         float top = s[qt][0][0];
 #pragma unroll
         for (int j = 1; j < 8; ++j) top = fmaxf(top, s[qt][j >> 2][j & 3]);
-        if (__ballot(top * sc > m[qt] + kRaiseAt)) {  // raise the reference: rare after the first tiles
+        if (__ballot((top - m[qt]) * sc > kRaiseAt)) {  // raise the reference: rare after the first tiles
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
-          const float up = fmaxf(m[qt], top * sc);
-          const float down = __builtin_amdgcn_exp2f(m[qt] - up);
+          const float up = fmaxf(m[qt], top);
+          const float down = __builtin_amdgcn_exp2f((m[qt] - up) * sc);
           m[qt] = up;
           l[qt] *= down;
 #pragma unroll
           for (int k = 0; k < kBlocks; ++k) o[qt][k] *= down;
         }
+        // c s - c m in one operation, unless c m is so large that its rounding shows: from 2^31 on the weights would overflow
+        float ref = m[qt] * sc;
+        if (__ballot(fabsf(ref) > 64.f)) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) s[qt][j >> 2][j & 3] -= m[qt];
+          ref = 0.f;
+        }
         u32x4 part0, part1, part2;
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
-          const float w0 = __builtin_amdgcn_exp2f(fmaf(s[qt][j >> 2][j & 3], sc, -m[qt]));
-          const float w1 = __builtin_amdgcn_exp2f(fmaf(s[qt][j >> 2][(j & 3) + 1], sc, -m[qt]));
+          const float w0 = __builtin_amdgcn_exp2f(fmaf(s[qt][j >> 2][j & 3], sc, -ref));
+          const float w1 = __builtin_amdgcn_exp2f(fmaf(s[qt][j >> 2][(j & 3) + 1], sc, -ref));
           l[qt] += w0 + w1;
           // A weight's bits eight at a time.  Where none are left, a part of a weight that is not 0 is the least bf16 number: the
           // parts of 0 alone are 0, and 0 times an infinite value is none.
@@ -499,7 +511,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
             for (int w = 0; w < kWays; ++w) top = fmaxf(top, part_stat[w][qt][n].x);
 #pragma unroll
             for (int w = 0; w < kWays; ++w) {
-              weight[w] = __builtin_amdgcn_exp2f(part_stat[w][qt][n].x - top);
+              weight[w] = __builtin_amdgcn_exp2f((part_stat[w][qt][n].x - top) * sc);
               sum += part_stat[w][qt][n].y * weight[w];
             }
           }
@@ -593,6 +605,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttention a, Layou
   __shared__ float sm[kSets], sl[kSets];
   __shared__ f32x4 so[kSets][kLanes];
   const int set = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+  const float sc = exponent_scale(a);
   float m = kNoMax, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   for (int p0 = set; p0 < join.y; p0 += kSets * kAhead) {
@@ -612,13 +625,13 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttention a, Layou
     }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) up = fmaxf(up, st[i].x);
-    const float keep = __builtin_amdgcn_exp2f(m - up);
+    const float keep = __builtin_amdgcn_exp2f((m - up) * sc);
     m = up;
     l *= keep;
     o *= keep;
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      const float w = __builtin_amdgcn_exp2f(st[i].x - up);
+      const float w = __builtin_amdgcn_exp2f((st[i].x - up) * sc);
       l += st[i].y * w;
       o += part[i] * w;
     }
@@ -635,11 +648,11 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttention a, Layou
   if (set > 0) return;
   float up = m;
   for (int i = 1; i < sets; ++i) up = fmaxf(up, sm[i]);
-  const float keep = __builtin_amdgcn_exp2f(m - up);
+  const float keep = __builtin_amdgcn_exp2f((m - up) * sc);
   l *= keep;
   o *= keep;
   for (int i = 1; i < sets; ++i) {
-    const float w = __builtin_amdgcn_exp2f(sm[i] - up);
+    const float w = __builtin_amdgcn_exp2f((sm[i] - up) * sc);
     l += sl[i] * w;
     o += so[i][lane] * w;
   }

@@ -145,3 +145,33 @@ def test_append_to_pools_that_lie_side_by_side(layout, heads, D, kv, n_pages):
         new = x.view(torch.int16).numpy() if dtype == BF else orc.quantise_e4m3(x.double().numpy(), 0)
         t.copy_(torch.from_numpy(po.paged_append(t.numpy(), new, slots)))
     assert torch.equal(on_gpu.cpu().view(want.dtype), want)
+
+
+@pytest.mark.parametrize("columns", [8, 80], ids=["whole", "cut"])
+@pytest.mark.parametrize("heads,kv_heads,D", [(16, 1, 128), (8, 4, 128), (32, 1, 128), (16, 4, 64), (48, 1, 64)])
+def test_attention_of_scores_far_beyond_the_range_of_weights(heads, kv_heads, D, columns):
+    # scores of 2^20 .. 2^80, each one exact product: the tokens of the highest share the weight equally, the others have none
+    n, tokens, page = 3, 64, 16
+    rng = np.random.default_rng(heads + D)
+    V = torch.zeros(n, columns * page, kv_heads, D)
+    V[:, torch.arange(tokens), :, torch.arange(tokens)] = 1.0
+    Vp = V.view(n * columns, page, kv_heads, D).to(BF).to(DEV)
+    for gain in (2.0 ** 20, 2.0 ** 31, 2.0 ** 40, 2.0 ** 80):
+        K, Q = torch.zeros(n, columns * page, kv_heads, D), torch.zeros(n, heads, D)
+        k0 = rng.integers(-127, 128, (n, tokens, kv_heads)) / 128.0
+        k0[:, 40:] = k0[:, 10:34]                                       # pairs, in one tile and in two
+        q0 = rng.integers(129, 256, (n, heads)) * rng.choice([-1, 1], (n, heads)) / 128.0 * gain
+        K[:, :tokens, :, 0], Q[:, :, 0] = torch.from_numpy(k0).float(), torch.from_numpy(q0).float()
+        Kp = K.view(n * columns, page, kv_heads, D).to(BF).to(DEV)
+        O = torch.empty(n, heads, D, dtype=torch.float32, device=DEV)
+        B.pafu_paged_attention(Q.to(BF).to(DEV), Kp, Vp, ints(np.arange(n * columns).reshape(n, columns)), ints([tokens] * n), O,
+                               softmax_scale=0.3, workspace=_workspace(n, heads, kv_heads, D))
+        s = q0[:, :, None] * np.repeat(k0.transpose(0, 2, 1), heads // kv_heads, axis=1)
+        best = s == s.max(-1, keepdims=True)
+        want = best / best.sum(-1, keepdims=True)                       # (the next one is gain / 2^14 * 0.3 below, 2^4 at least ...
+        w = np.exp(0.3 * (s - s.max(-1, keepdims=True)))
+        w /= w.sum(-1, keepdims=True)
+        assert np.abs(w - want).max() <= 2.0 ** -24                     # ... so this holds)
+        # weights 2^0 of exact differences, sums of at most 64 of them, a division and a product: as above without the scores' part
+        got = O.double().cpu().numpy()[:, :, :tokens]
+        assert np.abs(got - want).max() <= 40 * 2.0 ** -24, gain
